@@ -18,7 +18,8 @@ int check_quantize(const QuantizeProblem &p)
     if (p.rows < 0 || p.cols < 0 || p.count < 0 || !is_type(p.type)) return CONV_ERR_INVALID_ARG;
     if (p.take && (p.per_row <= 0 || p.src_rows < 0 || !on(p.take, 4))) return CONV_ERR_INVALID_ARG;
     if ((long long)p.cols * (p.gate ? 2 : 1) > p.lds || p.cols > 0x3fffffff) return CONV_ERR_INVALID_ARG;
-    if (!p.src || !on(p.src, size_of(p.type))) return CONV_ERR_INVALID_ARG;
+    const bool empty = p.take && p.src_rows == 0;   // (no row of the list is one then, and the source need not be there)
+    if ((!p.src && !empty) || !on(p.src, size_of(p.type))) return CONV_ERR_INVALID_ARG;
     if ((long long)blocks_of(p.cols) * ceil_div(p.rows, 16) * (p.count ? p.count : 1) > MOST_GRID) return CONV_ERR_UNSUPPORTED;
     return CONV_OK;
 }
@@ -89,7 +90,8 @@ int gemm_fp8_experts(int R, int a_rows, int E, int N, int K, const uint8_t *A, l
     if (rows ? per_row <= 0 : a_rows != R) return CONV_ERR_INVALID_ARG;
     if (!on(offsets, 4) || !on(rows, 4)) return CONV_ERR_INVALID_ARG;
     if (R == 0 || N == 0) return CONV_OK;
-    if (lda < K || ldw < K || ldc < N || a_rows == 0 || !C || !on(C, size_of(out_type))) return CONV_ERR_INVALID_ARG;
+    if (lda < K || ldw < K || ldc < N || !C || !on(C, size_of(out_type))) return CONV_ERR_INVALID_ARG;
+    if (a_rows == 0) K = 0;   // no row of the list is one: zeros, and no operand is read
     if (K > 0 && (!A || !sa || !W || !sw || !on(sa, 4) || !on(sw, 4))) return CONV_ERR_INVALID_ARG;
     if (R > 0x3fffffff || N > 0x3fffffff || a_rows > 0x3fffffff || K > 0x7fffff00) return CONV_ERR_UNSUPPORTED;
     if ((ceil_div(R, 16) + E + 1) * ceil_div(N, 16) > MOST_GRID * 8) return CONV_ERR_UNSUPPORTED;

@@ -1,0 +1,92 @@
+"""Routing to experts and block-scaled e4m3 products at the ends of their ranges: empty batches, limits, arguments, and which kernel a call takes."""
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from paper_2104_04731_amd import experts_fp8 as xp
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HOST = os.path.join(ROOT, "tests", "host")
+E4M3 = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    """What calls of the C entry points would launch (nothing runs)."""
+    from paper_2104_04731_amd import build
+    recorder = str(tmp_path_factory.mktemp("host") / "launch_recorder.so")
+    subprocess.run(["g++", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-I/opt/rocm/include", os.path.join(HOST, "launch_recorder.cpp"), "-o", recorder],
+                   check=True, timeout=300)
+
+    def run(calls):
+        r = subprocess.run([sys.executable, os.path.join(HOST, "experts_launches.py"), recorder, build.LIB, json.dumps(calls)], capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, r.stderr[-2000:]
+        return json.loads(r.stdout)
+    return run
+
+
+def experts_call(R, a_rows, E, N, K, rows=True, out_type=1, fast=0, lda=None, on16=True):
+    p = "p" if on16 else "odd"
+    return ["gemm_fp8_experts", [R, a_rows, E, N, K, p if a_rows else None, [lda or -(-K // 16) * 16], "p" if a_rows else None, p, [-(-K // 16) * 16], "p", "p",
+                                 "p" if rows else None, 2, "p", [N], out_type, fast, None]]
+
+
+# ---- no tokens --------------------------------------------------------------------------------------------------------
+def test_host_takes_a_list_of_rows_of_an_empty_source(launches):
+    """Every row of such a list is no row: zeros, from one launch.  Without a list there is still nothing that rows could be of."""
+    takes = [["quantize_fp8_rows", [256, 200, None, 1, [200], 0, "p", 2, 0, "p", [208], "p", None]],
+             ["quantize_fp8_columns", [256, 200, None, 1, [400], 1, "p", 2, 0, "p", [256], "p", None, [0], None, None]]]
+    takes += [experts_call(256, 0, 2, N, K, fast=fast) for N, K in ((130, 200), (4096, 1024), (16, 0)) for fast in (0, 1)]
+    assert [(c["rc"], c["launches"]) for c in launches(takes)] == [(0, 1)] * len(takes)
+    refused = [["quantize_fp8_rows", [256, 200, None, 1, [200], 0, None, 1, 0, "p", [208], "p", None]],
+               ["quantize_fp8_rows", [256, 200, None, 1, [200], 0, "p", 2, 3, "p", [208], "p", None]],
+               experts_call(256, 0, 2, 130, 200, rows=False)]
+    assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(1, 0)] * len(refused)
+
+
+def example():
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("experts_layer", os.path.join(ROOT, "examples", "experts_layer.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["rows", "columns", "rows+columns"])
+@pytest.mark.parametrize("gate", [False, True])
+def test_quantize_rows_of_an_empty_source(form, gate):
+    rows = torch.tensor([-1, 0, 7, -1, 5], dtype=torch.int32, device="cuda")
+    got = xp.quantize_fp8(torch.empty(0, 260 if gate else 130, device="cuda"), form=form, gate=gate, rows=rows, per_row=2)
+    assert got[0].shape == ((5, 130) if form.startswith("rows") else (130, 5))
+    for q, s in zip(got[::2], got[1::2]):
+        assert not q.float().any() and (s == 1).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,K", [(130, 200), (2056, 384)])
+def test_experts_of_an_empty_batch(N, K):
+    """Rows whose list names none: zeros, whatever lay in the result, rows of an expert and of none alike."""
+    w, sw = torch.ones(3, N, K, device="cuda").to(E4M3), torch.ones(3, -(-N // 128), -(-K // 128), device="cuda")
+    a, sa = torch.empty(0, K, dtype=E4M3, device="cuda"), torch.empty(-(-K // 128), 0, device="cuda")
+    for R in (9, 300, 3000):
+        rows, offsets = torch.arange(-1, R - 1, dtype=torch.int32, device="cuda"), torch.tensor([0, 2, 2, R - 5], dtype=torch.int32, device="cuda")
+        out = torch.full((R, N), 7.0, device="cuda")
+        xp.gemm_fp8_experts(a, sa, w, sw, offsets, rows=rows, dtype=torch.float32, out=out)
+        assert not out.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("align", [1, 128])
+def test_example_layer_without_tokens(align):
+    m = example()
+    x, logits, w1, w2, d_out = m.inputs(0, 4, 264, 136)
+    layer = m.Experts(w1, w2, 2, training=True)
+    out, saved = layer.forward(x, logits, align=align)
+    dx, dlogits, dw1, dw2 = layer.backward(d_out, saved)
+    assert out.shape == dx.shape == (0, 264) and dlogits.shape == (0, 4)
+    assert dw1.shape == (4, 272, 264) and dw2.shape == (4, 264, 136) and not dw1.any() and not dw2.any()
