@@ -6,6 +6,8 @@
  *     host, allocates, or needs a workspace, so every call may be captured into a HIP graph.
  *   - Every function returns a conv_status_t.  Arguments are validated before anything is enqueued.  Nothing throws.
  *     What only the device holds (ids, offsets, rows) is bounded by the kernels: a value out of range is no index.
+ *     Products whose extents pass 2^30 - 1 (summed ones 2^31 - 256) or whose results reach 2^24 tiles of 128 x 128 are
+ *     CONV_ERR_UNSUPPORTED.
  *   - Matrices are row-major; ld* is the distance of two rows in ELEMENTS, at least the row's length.  Any extent may be
  *     0 unless stated (nothing is read, results of an empty sum are zeros).
  *   - 8-bit values are OCP e4m3 (largest 448, no infinity).  Operands whose rows begin on 16 bytes are read fastest; any

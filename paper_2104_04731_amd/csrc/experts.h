@@ -102,6 +102,10 @@ struct Vec {
 #endif
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
+// A launch holds fewer than 2^32 lanes; what a problem that asks for more returns (CONV_ERR_UNSUPPORTED to the caller).
+constexpr hipError_t TOO_LARGE = hipErrorNotSupported;
+inline bool fits_launch(long long workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
+
 struct QuantizeProblem {
     const void *src;
     long long lds;

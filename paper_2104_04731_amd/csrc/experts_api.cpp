@@ -10,7 +10,7 @@ constexpr long long MOST_GRID = 0x7fffff;   // workgroups of 512 lanes within th
 bool is_type(int t) { return t == EXPERTS_F32 || t == EXPERTS_BF16 || t == EXPERTS_F16; }
 // The kernels read elements at their own alignment at least.
 bool on(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-int done(hipError_t e) { return e == hipSuccess ? CONV_OK : CONV_ERR_DEVICE; }
+int done(hipError_t e) { return e == hipSuccess ? CONV_OK : e == TOO_LARGE ? CONV_ERR_UNSUPPORTED : CONV_ERR_DEVICE; }
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
 int check_quantize(const QuantizeProblem &p)
@@ -78,7 +78,6 @@ int gemm_fp8_nt(int M, int N, int K, const uint8_t *A, long long lda, const floa
     if (lda < K || ldb < K || ldc < N || !C || !on(C, size_of(out_type))) return CONV_ERR_INVALID_ARG;
     if (K > 0 && (!A || !sa || !B || !sb || !on(sa, 4) || !on(sb, 4))) return CONV_ERR_INVALID_ARG;
     if (M > 0x3fffffff || N > 0x3fffffff || K > 0x7fffff00) return CONV_ERR_UNSUPPORTED;
-    if (ceil_div(M, 16) * ceil_div(N, 16) > MOST_GRID * 8) return CONV_ERR_UNSUPPORTED;
     Fp8Problem p{A, B, lda, ldb, ldc, sa, sb, C, M, N, K, M, b_rows != 0, out_type, 1, nullptr, nullptr, 1, fast_sums != 0};
     return done(launch_fp8_gemm(p, GEMM_DENSE, static_cast<hipStream_t>(stream)));
 }
@@ -94,7 +93,6 @@ int gemm_fp8_experts(int R, int a_rows, int E, int N, int K, const uint8_t *A, l
     if (a_rows == 0) K = 0;   // no row of the list is one: zeros, and no operand is read
     if (K > 0 && (!A || !sa || !W || !sw || !on(sa, 4) || !on(sw, 4))) return CONV_ERR_INVALID_ARG;
     if (R > 0x3fffffff || N > 0x3fffffff || a_rows > 0x3fffffff || K > 0x7fffff00) return CONV_ERR_UNSUPPORTED;
-    if ((ceil_div(R, 16) + E + 1) * ceil_div(N, 16) > MOST_GRID * 8) return CONV_ERR_UNSUPPORTED;
     Fp8Problem p{A, W, lda, ldw, ldc, sa, sw, C, R, N, K, a_rows, 0, out_type, E, offsets, rows, rows ? per_row : 1, fast_sums != 0};
     return done(launch_fp8_gemm(p, GEMM_EXPERTS, static_cast<hipStream_t>(stream)));
 }
@@ -108,7 +106,6 @@ int gemm_fp8_experts_grad(int R, int E, int N, int K, const uint8_t *A, long lon
     if (lda < R || ldb < R || ldc < K || !C || !on(C, size_of(out_type))) return CONV_ERR_INVALID_ARG;
     if (R > 0 && (!A || !sa || !B || !sb || !on(sa, 4) || !on(sb, 4))) return CONV_ERR_INVALID_ARG;
     if (R > 0x7fffff00 || N > 0x3fffffff || K > 0x3fffffff) return CONV_ERR_UNSUPPORTED;
-    if (ceil_div(N, 128) * ceil_div(K, 128) * E > MOST_GRID) return CONV_ERR_UNSUPPORTED;
     Fp8Problem p{A, B, lda, ldb, ldc, sa, sb, C, N, K, R, N, 1, out_type, E, offsets, nullptr, 1, fast_sums != 0};
     return done(launch_fp8_gemm(p, GEMM_GRAD, static_cast<hipStream_t>(stream)));
 }

@@ -735,13 +735,15 @@ long long slots_for(int R, int E, int rows)
     return (most < R ? most : R) + 1;
 }
 
+long long slots_of(const Fp8Problem &p, GemmKind kind, int rows) { return kind == GEMM_EXPERTS ? slots_for(p.M, p.E, rows) : (p.M + rows - 1) / rows; }
+long long tiles_of(const Fp8Problem &p, GemmKind kind, int rows, int cols) { return slots_of(p, kind, rows) * ((p.N + cols - 1) / cols) * (kind == GEMM_GRAD ? p.E : 1); }
+
 template <int TM, int TN, int WM, int WN, int PARTS, bool FAST>
 hipError_t launch_tiles(const Fp8Problem &p, GemmKind kind, Way way, hipStream_t st)
 {
     const int tiles_n = (p.N + TN - 1) / TN;
-    const long long slots = kind == GEMM_EXPERTS ? slots_for(p.M, p.E, TM) : (p.M + TM - 1) / TM;
-    const long long grid = slots * tiles_n * (kind == GEMM_GRAD ? p.E : 1);
-    if (grid > 0x7fffff) return hipErrorInvalidValue;
+    const long long slots = slots_of(p, kind, TM), grid = tiles_of(p, kind, TM, TN);
+    if (!fits_launch(grid, 64 * WM * WN * PARTS)) return TOO_LARGE;
     const dim3 g((unsigned)grid), b(64 * WM * WN * PARTS);
     const int s = (int)slots;
     if (kind == GEMM_EXPERTS) return c2i8::launch(fp8_tile_kernel<TM, TN, WM, WN, PARTS, GEMM_EXPERTS, false, FAST>, g, b, 0, st, p, s, tiles_n, way);
@@ -755,7 +757,7 @@ hipError_t launch_few(const Fp8Problem &p, GemmKind kind, long long slots, hipSt
 {
     constexpr int WIDTH = 16 * FEW_WAVES / SPLIT;
     const int tiles_n = (p.N + WIDTH - 1) / WIDTH;
-    if (slots * tiles_n > 0x7fffff) return hipErrorInvalidValue;
+    if (!fits_launch(slots * tiles_n, 64 * FEW_WAVES)) return TOO_LARGE;
     const dim3 g((unsigned)(slots * tiles_n)), b(64 * FEW_WAVES);
     const int s = (int)slots;
     if (kind == GEMM_EXPERTS) return c2i8::launch(fp8_few_kernel<MT, SPLIT, GEMM_EXPERTS, false>, g, b, 0, st, p, s, tiles_n);
@@ -765,7 +767,7 @@ hipError_t launch_few(const Fp8Problem &p, GemmKind kind, long long slots, hipSt
 template <int MT>
 hipError_t launch_few(const Fp8Problem &p, GemmKind kind, hipStream_t st)
 {
-    const long long slots = kind == GEMM_EXPERTS ? slots_for(p.M, p.E, 16 * MT) : (p.M + 16 * MT - 1) / (16 * MT);
+    const long long slots = slots_of(p, kind, 16 * MT);
     // the depth is shared out until there are 4096 waves, or as far as it goes
     const long long waves = slots * ((p.N + 15) / 16);
     if (waves >= 4096 || p.K <= 2 * BLOCK) return launch_few<MT, 1>(p, kind, slots, st);
@@ -802,7 +804,8 @@ hipError_t launch_fp8_gemm(const Fp8Problem &p, GemmKind kind, hipStream_t st)
     // 2048 x 2048 with 72 rows each 98 | 77 | 88, with 140 106 | 98 | 125, with 300 148 | 158 | 211.
     if (p.fast_sums && area >= 14e6 && rows >= 160 && depth >= (kind == GEMM_GRAD ? 4 : 8) && way == WAY_TRANSFERS)
         return launch_tiles<256, 256, 4, 2, 1, true>(p, kind, way, st);
-    if (area >= (kind == GEMM_EXPERTS ? 6e6 : 8e6) && rows > 64 && (p.fast_sums || depth >= 4))
+    // (and a launch need not hold as many of the smaller: 1024 weight gradients of 8192 x 8192 ask for 2^24)
+    if ((area >= (kind == GEMM_EXPERTS ? 6e6 : 8e6) && rows > 64 && (p.fast_sums || depth >= 4)) || !fits_launch(tiles_of(p, kind, 64, 64), 256))
         return p.fast_sums ? launch_tiles<128, 128, 2, 2, 1, true>(p, kind, way, st) : launch_tiles<128, 128, 2, 2, 1, false>(p, kind, way, st);
     // Tiles for no more than the compute units and a deep sum: in four parts to a workgroup, which bring in more at a time (us, one part | four: 300 x 1024,
     // depth 4096 13.4 | 10.1; 512 x 512, 8192 31 | 18.6; 512 x 512, 1024 5.6 | 5.7 and in 32 bits 7.3 | 6.9; of more tiles 1000 x 2048, 2048 10.0 | 13.9).

@@ -90,3 +90,29 @@ def test_example_layer_without_tokens(align):
     dx, dlogits, dw1, dw2 = layer.backward(d_out, saved)
     assert out.shape == dx.shape == (0, 264) and dlogits.shape == (0, 4)
     assert dw1.shape == (4, 272, 264) and dw2.shape == (4, 264, 136) and not dw1.any() and not dw2.any()
+
+
+# ---- limits -----------------------------------------------------------------------------------------------------------
+UNSUPPORTED = 2
+
+
+def grad_call(R, E, N, K, out_type=0, fast=0, on16=True, ld=None):
+    p, ld = "p" if on16 else "odd", ld or -(-R // 16) * 16
+    return ["gemm_fp8_experts_grad", [R, E, N, K, p, [ld], "p", p, [ld], "p", "p", "p", [K], out_type, fast, None]]
+
+
+def dense_call(M, N, K, b_rows=0, out_type=1, fast=0, on16=True, lda=None, ldb=None):
+    p, ld = "p" if on16 else "odd", -(-K // 16) * 16
+    return ["gemm_fp8_nt", [M, N, K, p, [lda or ld], "p", p, [ldb or ld], "p", b_rows, "p", [N], out_type, fast, None]]
+
+
+def test_host_products_that_small_tiles_would_not_hold(launches):
+    """A launch holds 2^32 lanes: results that ask for more in tiles of 64 x 64 take larger ones, those that ask for more in any are refused as such."""
+    most = 2 ** 30 - 1
+    takes = [grad_call(100000, 1024, 8192, 8192), grad_call(1000, 1024, 8192, 8192, fast=1), dense_call(most, 16, 128), dense_call(most, 16, 640, b_rows=1), dense_call(most, 100, 128, fast=1),
+             dense_call(16, most, 128), experts_call(2 ** 29, 2 ** 29, 3, 16, 128)]
+    for call in launches(takes):
+        assert (call["rc"], call["launches"]) == (0, 1) and 0 < call["workgroups"] * call["threads"] < 2 ** 32, call
+    refused = [grad_call(100000, 1024, 65536, 65536), grad_call(100000, 1024, 65536, 65536, fast=1), dense_call(most, most, 128), dense_call(most, most, 4096, fast=1, b_rows=1),
+               grad_call(100000, 1024, most, most), experts_call(most, most, 3, most, 128), experts_call(most, most, 1024, 65536, 4096, rows=False, fast=1)]
+    assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(UNSUPPORTED, 0)] * len(refused)
