@@ -96,7 +96,7 @@ int expert_rows(int pairs, int E, int align, const int32_t *ids, int32_t *offset
 
 /* ---- combination -----------------------------------------------------------------------------------------------------
  * out[t] = sum over j of weights[t][j] * y[place[t][j]], 32-bit sums; y [R][N]; weights f32 [T][k] or NULL for ones;
- * a place that is no row of y adds nothing.  out and y of one type. */
+ * a place that is no row of y adds nothing.  out and y of one type, out of up to 2^40 numbers (more: CONV_ERR_UNSUPPORTED). */
 int combine_experts(int T, int k, int N, int R, const void *y, long long ldy, int type, const int32_t *place, const float *weights,
                     void *out, long long ldo, void *stream);
 /* dy[r] = weights[p] * dout[p / k] for the pair p = rows[r] with place[p] = r, zeros for a row of no pair; dweights[p] = dout[p / k] . y[place[p]],

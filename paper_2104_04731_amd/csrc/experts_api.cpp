@@ -166,7 +166,7 @@ int combine_experts(int T, int k, int N, int R, const void *y, long long ldy, in
     const int size = size_of(type);
     if (ldo < N || (R > 0 && (!y || ldy < N || !on(y, size))) || !out || !place || !on(out, size) || !on(place, 4) || (weights && !on(weights, 4)))
         return CONV_ERR_INVALID_ARG;
-    if (ceil_div((long long)T * N, 256) > MOST_GRID) return CONV_ERR_UNSUPPORTED;
+    if ((long long)T * N > 1ll << 40) return CONV_ERR_UNSUPPORTED;
     CombineProblem p{T, k, N, R, type, y, nullptr, out, nullptr, ldy, 0, ldo, 0, place, nullptr, weights, nullptr};
     return done(launch_combine(p, static_cast<hipStream_t>(stream)));
 }

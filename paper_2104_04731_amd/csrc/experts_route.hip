@@ -411,11 +411,11 @@ __global__ __launch_bounds__(1024) void start_rows_kernel(OrderProblem p, int se
 // Combination: a thread on VEC neighbouring columns of a token; bound by the rows' bytes: 8192 tokens, 4 rows of 2048 bfloat16 each, in 40 us (168 MB, 4.2 TB/s), 32
 // tokens 3.8.
 template <typename T, int VEC>
-__global__ __launch_bounds__(256) void combine_kernel(CombineProblem p, int pieces)
+__global__ __launch_bounds__(256) void combine_kernel(CombineProblem p, int pieces, unsigned first)
 {
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long at = ((long long)first + blockIdx.x) * 256 + threadIdx.x;
+    if (at >= (long long)p.T * pieces) return;
     const int t = (int)(at / pieces), c = (int)(at % pieces) * VEC;
-    if (t >= p.T) return;
     const int32_t *place = p.place + (long long)t * p.k;
     const float *w = p.weights ? p.weights + (long long)t * p.k : nullptr;
     float sum[VEC] = {};
@@ -542,8 +542,14 @@ hipError_t launch_combine(const CombineProblem &p, hipStream_t st)
         constexpr int W = 16 / sizeof(T);
         const int pieces = vec ? p.N / W : p.N;
         const long long blocks = ((long long)p.T * pieces + 255) / 256;
-        return vec ? c2i8::launch(combine_kernel<T, W>, dim3((unsigned)blocks), dim3(256), 0, st, p, pieces)
-                   : c2i8::launch(combine_kernel<T, 1>, dim3((unsigned)blocks), dim3(256), 0, st, p, pieces);
+        constexpr long long MOST = 1 << 22;   // workgroups of a launch, 2^30 lanes; larger results take several
+        for (long long first = 0; first < blocks; first += MOST) {
+            const dim3 grid((unsigned)(blocks - first < MOST ? blocks - first : MOST));
+            const hipError_t e = vec ? c2i8::launch(combine_kernel<T, W>, grid, dim3(256), 0, st, p, pieces, (unsigned)first)
+                                     : c2i8::launch(combine_kernel<T, 1>, grid, dim3(256), 0, st, p, pieces, (unsigned)first);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     });
 }
 

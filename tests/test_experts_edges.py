@@ -116,3 +116,33 @@ def test_host_products_that_small_tiles_would_not_hold(launches):
     refused = [grad_call(100000, 1024, 65536, 65536), grad_call(100000, 1024, 65536, 65536, fast=1), dense_call(most, most, 128), dense_call(most, most, 4096, fast=1, b_rows=1),
                grad_call(100000, 1024, most, most), experts_call(most, most, 3, most, 128), experts_call(most, most, 1024, 65536, 4096, rows=False, fast=1)]
     assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(UNSUPPORTED, 0)] * len(refused)
+
+
+def combine_call(T, k, N, R, type=1, odd=False):
+    return ["combine_experts", [T, k, N, R, "odd" if odd else "p", [N], type, "p", "p", "p", [N], None]]
+
+
+def test_host_combines_results_of_2_to_the_31_and_more(launches):
+    """262144 tokens of 8192 bfloat16 are 4 GB; so are rows that are read element by element, which a launch has no lanes for: several then."""
+    takes = [(combine_call(262144, 8, 8192, 1000), 1), (combine_call(262144, 8, 8192, 1000, odd=True), 2), (combine_call(2 ** 24 + 1, 1, 64, 1000, odd=True), 2),
+             (combine_call(2 ** 30, 1, 64, 1000), 8), (combine_call(32, 6, 2048, 1000), 1)]
+    for (call, n), got in zip(takes, launches([c for c, _ in takes])):
+        assert (got["rc"], got["launches"]) == (0, n) and 0 < got["workgroups"] * got["threads"] <= 2 ** 30, (call, got)
+    refused = [combine_call(2 ** 31 - 1, 1, 2 ** 30, 1000)]
+    assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(UNSUPPORTED, 0)]
+
+
+@pytest.mark.gpu
+def test_combine_a_result_of_2_to_the_31():
+    """2^31 + 255 results, more than one launch where they go out element by element: the first and last tokens, and some around each power of two."""
+    T, N = 2 ** 24 + 1, 128
+    for odd in (0, 1):
+        y = torch.arange(5 * N, device="cuda").view(5, N).to(torch.bfloat16)
+        place = (torch.arange(T, device="cuda") % 5).int()[:, None].contiguous()
+        out = torch.zeros(T * N + odd, dtype=torch.bfloat16, device="cuda")[odd:].view(T, N)   # (rows that begin off 16 bytes go element by element)
+        xp.combine_experts(y, place, out=out)
+        at = torch.cat([torch.arange(max(0, c - 9), min(T, c + 9)) for c in [0, *(2 ** b for b in range(10, 25)), T]]).cuda()
+        assert torch.equal(out[at], y[at % 5])
+        for i in range(0, T, 2 ** 20):   # and all of them
+            part = out[i:i + 2 ** 20]
+            assert torch.equal(part, y[torch.arange(i, i + len(part), device="cuda") % 5])
