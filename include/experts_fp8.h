@@ -7,7 +7,7 @@
  *   - Every function returns a conv_status_t.  Arguments are validated before anything is enqueued.  Nothing throws.
  *     What only the device holds (ids, offsets, rows) is bounded by the kernels: a value out of range is no index.
  *     Products whose extents pass 2^30 - 1 (summed ones 2^31 - 256) or whose results reach 2^24 tiles of 128 x 128 are
- *     CONV_ERR_UNSUPPORTED.
+ *     CONV_ERR_UNSUPPORTED, as are over 2^25 - 4 tokens of a routing or pairs or rows of a combination's backward pass.
  *   - Matrices are row-major; ld* is the distance of two rows in ELEMENTS, at least the row's length.  Any extent may be
  *     0 unless stated (nothing is read, results of an empty sum are zeros).
  *   - 8-bit values are OCP e4m3 (largest 448, no infinity).  Operands whose rows begin on 16 bytes are read fastest; any
@@ -44,7 +44,8 @@ typedef enum {
  *     not NULL, what quantize_fp8_rows gives as well, from the same read
  * quantize_fp8_tiles  count matrices [rows][cols], each at src + i * rows * lds and q + i * (its rows) * ldq: a scale for 128 x 128;
  *     transpose == 0: q [rows][cols], scales [ceil(rows/128)][ceil(cols/128)]; != 0: both transposed
- * Scales are dense. */
+ * Scales are dense.  A launch takes rows of up to 2^30 - 1 and 2^24 - 1 pieces of 128 x 128, or of 16 rows x 512 columns (quantize_fp8_rows); more:
+ * CONV_ERR_UNSUPPORTED. */
 int quantize_fp8_rows(int rows, int cols, const void *src, int type, long long lds, int gate, const int32_t *take, int per_row, int src_rows,
                       uint8_t *q, long long ldq, float *scales, void *stream);
 int quantize_fp8_columns(int rows, int cols, const void *src, int type, long long lds, int gate, const int32_t *take, int per_row, int src_rows,

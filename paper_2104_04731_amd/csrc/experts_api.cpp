@@ -5,7 +5,7 @@ using namespace xp8;
 
 namespace {
 
-constexpr long long MOST_GRID = 0x7fffff;   // workgroups of 512 lanes within the 2^32 lanes of a launch
+constexpr long long MOST_GRID = 0x7fffff;   // workgroups of 256 lanes, half of what a launch holds
 
 bool is_type(int t) { return t == EXPERTS_F32 || t == EXPERTS_BF16 || t == EXPERTS_F16; }
 // The kernels read elements at their own alignment at least.
@@ -20,7 +20,7 @@ int check_quantize(const QuantizeProblem &p)
     if ((long long)p.cols * (p.gate ? 2 : 1) > p.lds || p.cols > 0x3fffffff) return CONV_ERR_INVALID_ARG;
     const bool empty = p.take && p.src_rows == 0;   // (no row of the list is one then, and the source need not be there)
     if ((!p.src && !empty) || !on(p.src, size_of(p.type))) return CONV_ERR_INVALID_ARG;
-    if ((long long)blocks_of(p.cols) * ceil_div(p.rows, 16) * (p.count ? p.count : 1) > MOST_GRID) return CONV_ERR_UNSUPPORTED;
+    if (p.rows > 0x3fffffff) return CONV_ERR_UNSUPPORTED;
     return CONV_OK;
 }
 

@@ -457,18 +457,22 @@ hipError_t for_source(const QuantizeProblem &p, F &&f)
 hipError_t launch_quantize_rows(const QuantizeProblem &p, hipStream_t st)
 {
     const long long across = (p.cols + ROWS_COLS - 1) / ROWS_COLS;
+    const long long large = across * ((p.rows + 15) / 16);
+    if (!fits_launch(large, 256)) return TOO_LARGE;
     return for_source(p, [&](auto t, auto vec, auto gate) {
         using T = decltype(t);
         // four rows a wave hide the loads' time; until there are four workgroups for every compute unit one row, so that there are more of them
-        if (across * ((p.rows + 15) / 16) >= 1024)
-            return c2i8::launch(quantize_rows_kernel<T, vec.value, gate.value, 4>, dim3((unsigned)(across * ((p.rows + 15) / 16))), dim3(256), 0, st, p);
+        if (large >= 1024)
+            return c2i8::launch(quantize_rows_kernel<T, vec.value, gate.value, 4>, dim3((unsigned)large), dim3(256), 0, st, p);
         return c2i8::launch(quantize_rows_kernel<T, vec.value, gate.value, 1>, dim3((unsigned)(across * ((p.rows + 3) / 4))), dim3(256), 0, st, p);
     });
 }
 
 hipError_t launch_quantize_columns(const QuantizeProblem &p, hipStream_t st)
 {
-    const dim3 grid((unsigned)blocks_of(p.cols) * (unsigned)blocks_of(p.rows));
+    const long long tiles = (long long)blocks_of(p.cols) * blocks_of(p.rows);
+    if (!fits_launch(tiles, 256)) return TOO_LARGE;
+    const dim3 grid((unsigned)tiles);
     return for_source(p, [&](auto t, auto vec, auto gate) {
         return c2i8::launch(quantize_tile_kernel<decltype(t), vec.value, gate.value, true>, grid, dim3(256), 0, st, p);
     });
@@ -476,7 +480,9 @@ hipError_t launch_quantize_columns(const QuantizeProblem &p, hipStream_t st)
 
 hipError_t launch_quantize_tiles(const QuantizeProblem &p, hipStream_t st)
 {
-    const dim3 grid((unsigned)blocks_of(p.cols) * (unsigned)blocks_of(p.rows) * (unsigned)p.count);
+    const long long tiles = (long long)blocks_of(p.cols) * blocks_of(p.rows);
+    if (!fits_launch(tiles, 256) || !fits_launch(tiles * p.count, 256)) return TOO_LARGE;
+    const dim3 grid((unsigned)(tiles * p.count));
     const bool vec = in_pieces(p.src, p.lds, p.cols, size_of(p.type));
     return with_type(p.type, [&](auto t) {
         using T = decltype(t);

@@ -146,3 +146,20 @@ def test_combine_a_result_of_2_to_the_31():
         for i in range(0, T, 2 ** 20):   # and all of them
             part = out[i:i + 2 ** 20]
             assert torch.equal(part, y[torch.arange(i, i + len(part), device="cuda") % 5])
+
+
+def test_host_quantises_as_many_blocks_as_a_launch_holds(launches):
+    """The limit is the launch's: 16 rows by 512 columns to a workgroup by rows, 128 x 128 otherwise."""
+    def rows(r, c):
+        return ["quantize_fp8_rows", [r, c, "p", 1, [c], 0, None, 1, 0, "p", [c], "p", None]]
+
+    def columns(r, c):
+        return ["quantize_fp8_columns", [r, c, "p", 1, [c], 0, None, 1, 0, "p", [r], "p", None, [0], None, None]]
+
+    def tiles(n, r, c):
+        return ["quantize_fp8_tiles", [n, r, c, "p", 1, [c], 0, "p", [c], "p", None]]
+    takes = [(rows(2 ** 21, 16384), 2 ** 17 * 32), (columns(2 ** 20, 32768), 2 ** 13 * 256), (tiles(1024, 16384, 4096), 1024 * 128 * 32), (rows(2 ** 27, 512), 2 ** 23)]
+    for (call, n), got in zip(takes, launches([c for c, _ in takes])):
+        assert (got["rc"], got["launches"], got["workgroups"]) == (0, 1, n), (call, got)
+    refused = [rows(2 ** 30, 512), rows(2 ** 31 - 1, 1), columns(2 ** 30, 512), columns(2 ** 31 - 1, 1), tiles(1024, 2 ** 20, 2 ** 20), tiles(2 ** 30, 2 ** 30, 2 ** 29)]
+    assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(UNSUPPORTED, 0)] * len(refused)
