@@ -5,6 +5,7 @@
 #include <vector>
 
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/util/SmallVector.h>
 
 #include "../../include/experts_fp8.h"
@@ -68,6 +69,9 @@ struct Call {
     const at::Tensor &on_device(const at::Tensor &t, const char *what)
     {
         if (!t.is_cuda()) refuse(PyExc_TypeError, "%s must be a CUDA tensor", what);
+        // (a result that autograd knows nothing of must not stand in for one that it does)
+        if (t.requires_grad() && c10::GradMode::is_enabled())
+            refuse(PyExc_ValueError, "%s requires a gradient, which this call does not record: call it under torch.no_grad() or in an autograd.Function", what);
         if (device < 0) {
             device = t.get_device();
             if (device != stream.device_index()) refuse(PyExc_ValueError, "%s is on device %d, the stream on device %d", what, device, (int)stream.device_index());

@@ -4,6 +4,9 @@ Same names and manner as `binding`: arguments are marshalled, nothing is compute
 stream, or the caller's (`out`); a call the library refuses raises `binding.ConvError`, a tensor of the wrong type or shape
 TypeError or ValueError.  Matrices are row-major with neighbouring elements in a row; rows may lie further apart.  New 8-bit
 results have rows that begin on 16 bytes (the distance of two rows is a multiple of 16), which is what the products read fastest.
+
+Gradients are calls of their own (`..._backward`, `gemm_fp8_experts_grad`, and for the products the products themselves); autograd records none of these calls.  A tensor
+that requires a gradient is refused with ValueError while autograd records: call under `torch.no_grad()`, or in the forward and backward of an `autograd.Function`.
 """
 from __future__ import annotations
 

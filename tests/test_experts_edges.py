@@ -163,3 +163,58 @@ def test_host_quantises_as_many_blocks_as_a_launch_holds(launches):
         assert (got["rc"], got["launches"], got["workgroups"]) == (0, 1, n), (call, got)
     refused = [rows(2 ** 30, 512), rows(2 ** 31 - 1, 1), columns(2 ** 30, 512), columns(2 ** 31 - 1, 1), tiles(1024, 2 ** 20, 2 ** 20), tiles(2 ** 30, 2 ** 30, 2 ** 29)]
     assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(UNSUPPORTED, 0)] * len(refused)
+
+
+# ---- gradients are calls of their own -----------------------------------------------------------------------------------
+def differentiable_calls():
+    """(name, call of one tensor, that tensor) for each floating-point argument that a program could differentiate by."""
+    x, y, d = torch.randn(4, 8, device="cuda"), torch.randn(8, 16, device="cuda"), torch.randn(4, 16, device="cuda")
+    ids, w = xp.route_experts(x, 2)
+    off, rows, place = xp.expert_rows(ids, 8)
+    q, s = xp.quantize_fp8(y)
+    return [("route_experts", lambda v: xp.route_experts(v, 2), x), ("route_experts bias", lambda v: xp.route_experts(x, 2, bias=v), torch.zeros(8, device="cuda")),
+            ("route_experts_backward", lambda v: xp.route_experts_backward(v, ids, x), w), ("quantize_fp8", xp.quantize_fp8, y),
+            ("silu_gate_backward", lambda v: xp.silu_gate_backward(y, v), torch.randn(8, 8, device="cuda")), ("gemm_fp8_nt scales", lambda v: xp.gemm_fp8_nt(q, v, q, s, b_rows=True), s),
+            ("combine_experts", lambda v: xp.combine_experts(v, place, w), y), ("combine_experts weights", lambda v: xp.combine_experts(y, place, v), w),
+            ("combine_experts_backward", lambda v: xp.combine_experts_backward(v, y, place, rows, w), d)]
+
+
+@pytest.mark.gpu
+def test_inputs_that_ask_for_a_gradient_are_refused():
+    """A result without a gradient must not come back where autograd would record one; without recording the calls run and give what they give."""
+    for name, call, v in differentiable_calls():
+        plain = call(v)
+        asks = v.detach().clone().requires_grad_()
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(asks)
+        with torch.no_grad():
+            again = call(asks)
+        for a, b in zip(plain if isinstance(plain, tuple) else (plain,), again if isinstance(again, tuple) else (again,)):
+            assert torch.equal(a.view(torch.uint8) if a.dtype == E4M3 else a, b.view(torch.uint8) if b.dtype == E4M3 else b), name
+
+
+@pytest.mark.gpu
+def test_calls_within_a_function_of_autograd():
+    """How a program joins a call and its gradient: the combination, whose sums are linear in rows and weights."""
+    ids, w = xp.route_experts(torch.randn(5, 8, device="cuda"), 3)
+    off, rows, place = xp.expert_rows(ids, 8)
+
+    class Combine(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, y, w):
+            ctx.save_for_backward(y, w)
+            return xp.combine_experts(y, place, w)
+
+        @staticmethod
+        def backward(ctx, d):
+            y, w = ctx.saved_tensors
+            return xp.combine_experts_backward(d.contiguous(), y, place, rows, w)
+    y, w = torch.randn(15, 16, device="cuda").requires_grad_(), w.requires_grad_()
+    d = torch.randn(5, 16, device="cuda")
+    (Combine.apply(y, w) * d).sum().backward()
+    got = y.grad.clone(), w.grad.clone()
+    y64, w64 = y.detach().double().requires_grad_(), w.detach().double().requires_grad_()
+    ((w64[:, :, None] * y64[place.long()]).sum(1) * d.double()).sum().backward()
+    terms = (d.double().abs()[:, None] * y64.detach()[place.long()].abs()).sum(2)
+    for a, b, bound in zip(got, (y64.grad, w64.grad), (y64.grad.abs(), 18 * terms)):   # one product; a sum of 16
+        assert ((a.double() - b).abs() <= 2.0 ** -23 * bound).all()
