@@ -34,6 +34,18 @@ template <class... A>
     throw PyFail{};
 }
 
+// A call of the library, the interpreter lock given up for it (the arguments' checks are done by then).
+template <class... P, class... A>
+void run(const char *what, int (*call)(P...), A... a)
+{
+    int rc;
+    {
+        NoGil unlocked;
+        rc = call(static_cast<P>(a)...);
+    }
+    check(rc, what);
+}
+
 int type_of(at::ScalarType t)   // -1: none of the three
 {
     return t == at::kFloat ? EXPERTS_F32 : t == at::kBFloat16 ? EXPERTS_BF16 : t == at::kHalf ? EXPERTS_F16 : -1;
@@ -141,6 +153,7 @@ struct Results {
             for (int i = (int)shape.size() - 3; i >= 0; --i) strides[i] = strides[i + 1] * shape[i + 1];
             if (other) c10::hip::setCurrentHIPStream(call.stream);
             try {
+                NoGil unlocked;
                 made.push_back(at::detail::empty_strided_cuda(shape, strides, type, like.device()));   // (without the dispatcher: half the time)
             } catch (...) {
                 if (other) c10::hip::setCurrentHIPStream(now);
@@ -205,7 +218,6 @@ NATIVE(quantize_fp8, 7, {
     const int cols = as_extent(x.size(-1), "x") / (gate ? 2 : 1);
     const int32_t *at_rows = take ? (const int32_t *)take->data_ptr() : nullptr;
     Results out(call, a[5], form == BOTH ? 4 : 2);
-    int rc;
     if (tiles) {
         const bool turned = form == TILES_T;
         const int64_t r = turned ? cols : rows, c = turned ? rows : cols;
@@ -214,8 +226,7 @@ NATIVE(quantize_fp8, 7, {
         const at::Tensor q = out.next(shape, at::kFloat8_e4m3fn, whole16(c), x, "values"), s = out.dense(blocks, at::kFloat, x, "scales");
         const int64_t ldq = row_distance(q, "values");
         if (dims == 3 && count > 1 && q.stride(0) != r * ldq) refuse(PyExc_ValueError, "the matrices of the values must follow one another");
-        rc = lib.quantize_fp8_tiles(as_extent(count, "x"), rows, cols, x.data_ptr(), type, ld, turned, (uint8_t *)q.data_ptr(), ldq, (float *)s.data_ptr(), call.handle());
-        check(rc, "quantize_fp8_tiles");
+        run("quantize_fp8_tiles", lib.quantize_fp8_tiles, as_extent(count, "x"), rows, cols, x.data_ptr(), type, ld, turned, (uint8_t *)q.data_ptr(), ldq, (float *)s.data_ptr(), call.handle());
         return out.result();
     }
     at::Tensor q;
@@ -225,18 +236,16 @@ NATIVE(quantize_fp8, 7, {
         s = out.dense({blocks_of(cols), rows}, at::kFloat, x, "scales");
     }
     if (form == ROWS) {
-        rc = lib.quantize_fp8_rows(rows, cols, x.data_ptr(), type, ld, gate, at_rows, per_row, src_rows, (uint8_t *)q.data_ptr(), row_distance(q, "values"),
-                                   (float *)s.data_ptr(), call.handle());
-        check(rc, "quantize_fp8_rows");
+        run("quantize_fp8_rows", lib.quantize_fp8_rows, rows, cols, x.data_ptr(), type, ld, gate, at_rows, per_row, src_rows, (uint8_t *)q.data_ptr(), row_distance(q, "values"),
+            (float *)s.data_ptr(), call.handle());
         return out.result();
     }
     const at::Tensor qt = out.next({cols, rows}, at::kFloat8_e4m3fn, whole16(rows), x, "transposed values");
     const at::Tensor st = out.dense({blocks_of(rows), cols}, at::kFloat, x, "columns' scales");
     const bool both = form == BOTH;
-    rc = lib.quantize_fp8_columns(rows, cols, x.data_ptr(), type, ld, gate, at_rows, per_row, src_rows, (uint8_t *)qt.data_ptr(),
-                                  row_distance(qt, "transposed values"), (float *)st.data_ptr(), both ? (uint8_t *)q.data_ptr() : nullptr,
-                                  both ? row_distance(q, "values") : 0, both ? (float *)s.data_ptr() : nullptr, call.handle());
-    check(rc, "quantize_fp8_columns");
+    run("quantize_fp8_columns", lib.quantize_fp8_columns, rows, cols, x.data_ptr(), type, ld, gate, at_rows, per_row, src_rows, (uint8_t *)qt.data_ptr(),
+        row_distance(qt, "transposed values"), (float *)st.data_ptr(), both ? (uint8_t *)q.data_ptr() : nullptr,
+        both ? row_distance(q, "values") : 0, both ? (float *)s.data_ptr() : nullptr, call.handle());
     return out.result();
 })
 
@@ -250,9 +259,8 @@ NATIVE(silu_gate_backward, 4, {
     const int rows = as_extent(x.size(0), "x"), cols = as_extent(dh.size(1), "dh");
     Results out(call, a[2], 1);
     const at::Tensor dx = out.next({rows, 2 * (int64_t)cols}, x.scalar_type(), 0, x, "out");
-    check(lib.silu_gate_backward(rows, cols, x.data_ptr(), row_distance(x, "x"), dh.data_ptr(), row_distance(dh, "dh"), dx.data_ptr(), row_distance(dx, "out"), type,
-                                 call.handle()),
-          "silu_gate_backward");
+    run("silu_gate_backward", lib.silu_gate_backward, rows, cols, x.data_ptr(), row_distance(x, "x"), dh.data_ptr(), row_distance(dh, "dh"), dx.data_ptr(), row_distance(dx, "out"), type,
+        call.handle());
     return out.result();
 })
 
@@ -277,9 +285,8 @@ NATIVE(gemm_fp8_nt, 9, {
     const at::ScalarType dtype = as_dtype(a[5]);
     Results out(call, a[7], 1);
     const at::Tensor C = out.next({M, N}, dtype, 0, A, "out");
-    check(lib.gemm_fp8_nt(M, N, K, (const uint8_t *)A.data_ptr(), row_distance(A, "a"), (const float *)sa.data_ptr(), (const uint8_t *)B.data_ptr(),
-                          row_distance(B, "b"), (const float *)sb.data_ptr(), b_rows, C.data_ptr(), row_distance(C, "out"), type_of(dtype), fast_sums, call.handle()),
-          "gemm_fp8_nt");
+    run("gemm_fp8_nt", lib.gemm_fp8_nt, M, N, K, (const uint8_t *)A.data_ptr(), row_distance(A, "a"), (const float *)sa.data_ptr(), (const uint8_t *)B.data_ptr(),
+        row_distance(B, "b"), (const float *)sb.data_ptr(), b_rows, C.data_ptr(), row_distance(C, "out"), type_of(dtype), fast_sums, call.handle());
     return out.result();
 })
 
@@ -304,10 +311,9 @@ NATIVE(gemm_fp8_experts, 11, {
     const at::ScalarType dtype = as_dtype(a[7]);
     Results out(call, a[9], 1);
     const at::Tensor C = out.next({R, N}, dtype, 0, A, "out");
-    check(lib.gemm_fp8_experts(R, a_rows, E, N, K, (const uint8_t *)A.data_ptr(), row_distance(A, "a"), (const float *)sa.data_ptr(), (const uint8_t *)W.data_ptr(),
-                               ldw, (const float *)sw.data_ptr(), (const int32_t *)offsets.data_ptr(), rows ? (const int32_t *)rows->data_ptr() : nullptr, per_row,
-                               C.data_ptr(), row_distance(C, "out"), type_of(dtype), fast_sums, call.handle()),
-          "gemm_fp8_experts");
+    run("gemm_fp8_experts", lib.gemm_fp8_experts, R, a_rows, E, N, K, (const uint8_t *)A.data_ptr(), row_distance(A, "a"), (const float *)sa.data_ptr(), (const uint8_t *)W.data_ptr(),
+        ldw, (const float *)sw.data_ptr(), (const int32_t *)offsets.data_ptr(), rows ? (const int32_t *)rows->data_ptr() : nullptr, per_row,
+        C.data_ptr(), row_distance(C, "out"), type_of(dtype), fast_sums, call.handle());
     return out.result();
 })
 
@@ -328,9 +334,8 @@ NATIVE(gemm_fp8_experts_grad, 9, {
     const at::Tensor C = out.next({E, N, K}, dtype, 0, A, "out");
     const int64_t ldc = row_distance(C, "out");
     if (E > 1 && C.stride(0) != N * ldc) refuse(PyExc_ValueError, "the matrices of out must follow one another");
-    check(lib.gemm_fp8_experts_grad(R, E, N, K, (const uint8_t *)A.data_ptr(), row_distance(A, "a"), (const float *)sa.data_ptr(), (const uint8_t *)B.data_ptr(),
-                                    row_distance(B, "b"), (const float *)sb.data_ptr(), (const int32_t *)off.data_ptr(), C.data_ptr(), ldc, type_of(dtype), fast_sums, call.handle()),
-          "gemm_fp8_experts_grad");
+    run("gemm_fp8_experts_grad", lib.gemm_fp8_experts_grad, R, E, N, K, (const uint8_t *)A.data_ptr(), row_distance(A, "a"), (const float *)sa.data_ptr(), (const uint8_t *)B.data_ptr(),
+        row_distance(B, "b"), (const float *)sb.data_ptr(), (const int32_t *)off.data_ptr(), C.data_ptr(), ldc, type_of(dtype), fast_sums, call.handle());
     return out.result();
 })
 
@@ -352,9 +357,8 @@ NATIVE(route_experts, 11, {
     if (k < 1) fail(CONV_ERR_INVALID_ARG, "route_experts");
     Results out(call, a[9], 2);
     const at::Tensor ids = out.dense({T, k}, at::kInt, x, "ids"), weights = out.dense({T, k}, at::kFloat, x, "weights");
-    check(lib.route_experts(T, E, k, x.data_ptr(), type, row_distance(x, "logits"), bias ? (const float *)bias->data_ptr() : nullptr, sigmoid, groups, kept, group_top,
-                            renormalise, factor, (int32_t *)ids.data_ptr(), (float *)weights.data_ptr(), call.handle()),
-          "route_experts");
+    run("route_experts", lib.route_experts, T, E, k, x.data_ptr(), type, row_distance(x, "logits"), bias ? (const float *)bias->data_ptr() : nullptr, sigmoid, groups, kept, group_top,
+        renormalise, factor, (int32_t *)ids.data_ptr(), (float *)weights.data_ptr(), call.handle());
     return out.result();
 })
 
@@ -370,9 +374,8 @@ NATIVE(route_experts_backward, 8, {
     const float factor = as_float(a[5]);
     Results out(call, a[6], 1);
     const at::Tensor dx = out.next({T, E}, x.scalar_type(), 0, x, "out");
-    check(lib.route_experts_backward(T, E, k, x.data_ptr(), type, row_distance(x, "logits"), (const int32_t *)ids.data_ptr(), (const float *)dw.data_ptr(), sigmoid,
-                                     renormalise, factor, dx.data_ptr(), row_distance(dx, "out"), call.handle()),
-          "route_experts_backward");
+    run("route_experts_backward", lib.route_experts_backward, T, E, k, x.data_ptr(), type, row_distance(x, "logits"), (const int32_t *)ids.data_ptr(), (const float *)dw.data_ptr(), sigmoid,
+        renormalise, factor, dx.data_ptr(), row_distance(dx, "out"), call.handle());
     return out.result();
 })
 
@@ -387,9 +390,8 @@ NATIVE(expert_rows, 5, {
     Results out(call, a[3], 3);
     const at::Tensor offsets = out.dense({E + 1}, at::kInt, ids, "offsets"), rows = out.dense({R}, at::kInt, ids, "rows"),
                      place = out.dense(ids.sizes(), at::kInt, ids, "place");
-    check(lib.expert_rows(pairs, E, align, (const int32_t *)ids.data_ptr(), (int32_t *)offsets.data_ptr(), (int32_t *)rows.data_ptr(), (int32_t *)place.data_ptr(),
-                          call.handle()),
-          "expert_rows");
+    run("expert_rows", lib.expert_rows, pairs, E, align, (const int32_t *)ids.data_ptr(), (int32_t *)offsets.data_ptr(), (int32_t *)rows.data_ptr(), (int32_t *)place.data_ptr(),
+        call.handle());
     return out.result();
 })
 
@@ -404,9 +406,8 @@ NATIVE(combine_experts, 5, {
     const at::Tensor *w = a[2] == Py_None ? nullptr : &call.dense(a[2], at::kFloat, {T, k}, "weights");
     Results out(call, a[3], 1);
     const at::Tensor o = out.next({T, N}, y.scalar_type(), 0, y, "out");
-    check(lib.combine_experts(T, k, N, R, y.data_ptr(), row_distance(y, "y"), type, (const int32_t *)place.data_ptr(), w ? (const float *)w->data_ptr() : nullptr,
-                              o.data_ptr(), row_distance(o, "out"), call.handle()),
-          "combine_experts");
+    run("combine_experts", lib.combine_experts, T, k, N, R, y.data_ptr(), row_distance(y, "y"), type, (const int32_t *)place.data_ptr(), w ? (const float *)w->data_ptr() : nullptr,
+        o.data_ptr(), row_distance(o, "out"), call.handle());
     return out.result();
 })
 
@@ -424,10 +425,9 @@ NATIVE(combine_experts_backward, 7, {
     const at::Tensor *w = a[4] == Py_None ? nullptr : &call.dense(a[4], at::kFloat, {T, k}, "weights");
     Results out(call, a[5], 2);
     const at::Tensor dy = out.next({R, N}, y.scalar_type(), 0, y, "out[0]"), dw = out.dense({T, k}, at::kFloat, y, "out[1]");
-    check(lib.combine_experts_backward(T, k, N, R, d.data_ptr(), row_distance(d, "dout"), y.data_ptr(), row_distance(y, "y"), type, (const int32_t *)place.data_ptr(),
-                                       (const int32_t *)rows.data_ptr(), w ? (const float *)w->data_ptr() : nullptr, dy.data_ptr(), row_distance(dy, "out[0]"),
-                                       (float *)dw.data_ptr(), call.handle()),
-          "combine_experts_backward");
+    run("combine_experts_backward", lib.combine_experts_backward, T, k, N, R, d.data_ptr(), row_distance(d, "dout"), y.data_ptr(), row_distance(y, "y"), type, (const int32_t *)place.data_ptr(),
+        (const int32_t *)rows.data_ptr(), w ? (const float *)w->data_ptr() : nullptr, dy.data_ptr(), row_distance(dy, "out[0]"),
+        (float *)dw.data_ptr(), call.handle());
     return out.result();
 })
 

@@ -218,3 +218,42 @@ def test_calls_within_a_function_of_autograd():
     terms = (d.double().abs()[:, None] * y64.detach()[place.long()].abs()).sum(2)
     for a, b, bound in zip(got, (y64.grad, w64.grad), (y64.grad.abs(), 18 * terms)):   # one product; a sum of 16
         assert ((a.double() - b).abs() <= 2.0 ** -23 * bound).all()
+
+
+# ---- other threads ------------------------------------------------------------------------------------------------------
+@pytest.fixture
+def stand_in(tmp_path):
+    """The library's entry points replaced by ones that do nothing but note whether their caller holds the interpreter lock; yields the notes."""
+    import ctypes
+
+    from paper_2104_04731_amd import binding
+    names = sorted({*binding.EXPORTS, *xp.EXPORTS} - {"expert_rows_capacity"})
+    source = tmp_path / "stand_in.cpp"
+    source.write_text('#include <dlfcn.h>\nextern "C" {\nint notes[2];\nstatic int note() { ++notes[((int (*)())dlsym(RTLD_DEFAULT, "PyGILState_Check"))() ? 1 : 0]; return 0; }\n'
+                      "int expert_rows_capacity(int pairs, int, int) { return pairs; }\n" + "".join(f"int {n}() {{ return note(); }}\n" for n in names) + "}\n")
+    subprocess.run(["g++", "-shared", "-fPIC", str(source), "-o", str(tmp_path / "stand_in.so"), "-ldl"], check=True, timeout=120)
+    native = binding._calls()
+    other = ctypes.CDLL(str(tmp_path / "stand_in.so"))
+    native.set_library(other._handle)
+    try:
+        yield (ctypes.c_int * 2).in_dll(other, "notes")
+    finally:
+        native.set_library(binding._lib._handle)
+
+
+@pytest.mark.gpu
+def test_calls_give_up_the_interpreter_lock(stand_in):
+    """Other threads run while a call launches, as with every other call that takes tensors."""
+    x, half = torch.zeros(4, 256, device="cuda"), torch.zeros(4, 128, device="cuda")
+    q, s, w, sw = torch.zeros(4, 256, device="cuda").to(E4M3), torch.ones(2, 4, device="cuda"), torch.zeros(2, 6, 256, device="cuda").to(E4M3), torch.ones(2, 1, 2, device="cuda")
+    qt, st = torch.zeros(6, 4, device="cuda").to(E4M3), torch.ones(1, 6, device="cuda")
+    ids, weights, off = torch.zeros(4, 2, dtype=torch.int32, device="cuda"), torch.ones(4, 2, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    rows, out = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.empty(4, 4, dtype=torch.bfloat16, device="cuda")
+    calls = [lambda form=form: xp.quantize_fp8(x, form=form) for form in xp.FORMS]
+    calls += [lambda: xp.silu_gate_backward(x, half), lambda: xp.gemm_fp8_nt(q, s, q, s, b_rows=True), lambda: xp.gemm_fp8_nt(q, s, q, s, b_rows=True, out=out),
+              lambda: xp.gemm_fp8_experts(q, s, w, sw, off), lambda: xp.gemm_fp8_experts_grad(qt, st, qt, st, off), lambda: xp.route_experts(half, 2),
+              lambda: xp.route_experts_backward(weights, ids, half), lambda: xp.expert_rows(ids, 4), lambda: xp.combine_experts(x, ids, weights),
+              lambda: xp.combine_experts_backward(x, x, ids, rows, weights)]
+    for i, call in enumerate(calls):
+        call()
+        assert list(stand_in) == [i + 1, 0], i
