@@ -62,6 +62,18 @@ int as_extent(int64_t n, const char *what)
     return (int)n;
 }
 
+// A whole number (as_int takes them modulo 2^32, as its callers always have)
+int whole(PyObject *o, const char *what)
+{
+    PyObject *i = PyNumber_Index(o);
+    if (!i) throw PyFail{};
+    int over = 0;
+    const long v = PyLong_AsLongAndOverflow(i, &over);
+    Py_DECREF(i);
+    if (over || v != (int)v) refuse(PyExc_ValueError, "%s is out of range", what);
+    return (int)v;
+}
+
 // The call's device (the first tensor's, which must be the current one) and stream.  Results are allocated for the stream that the call runs on.
 struct Call {
     int device = -1;
@@ -202,7 +214,7 @@ NATIVE(quantize_fp8, 7, {
     const bool tiles = form >= TILES;
     const int dims = tiles && tensor(a[0], "x").dim() == 3 ? 3 : 2;
     const at::Tensor &x = call.rows(a[0], dims, "x");
-    const int type = type_of(x, "x"), gate = as_bool(a[2]), per_row = as_int(a[4]);
+    const int type = type_of(x, "x"), gate = as_bool(a[2]), per_row = whole(a[4], "per_row");
     if (gate && tiles) refuse(PyExc_ValueError, "a gated activation has no form \"tiles\"");
     if (gate && x.size(-1) % 2) refuse(PyExc_ValueError, "x must have an even number of columns with a gate");
     const at::Tensor *take = nullptr;
@@ -307,7 +319,7 @@ NATIVE(gemm_fp8_experts, 11, {
         rows = &call.on_device(tensor(a[5], "rows"), "rows");
         if (rows->scalar_type() != at::kInt || rows->dim() != 1 || !rows->is_contiguous()) refuse(PyExc_TypeError, "rows must be a contiguous int32 vector");
     }
-    const int R = rows ? as_extent(rows->size(0), "rows") : a_rows, per_row = as_int(a[6]);
+    const int R = rows ? as_extent(rows->size(0), "rows") : a_rows, per_row = whole(a[6], "per_row");
     const at::ScalarType dtype = as_dtype(a[7]);
     Results out(call, a[9], 1);
     const at::Tensor C = out.next({R, N}, dtype, 0, A, "out");
@@ -350,11 +362,11 @@ float as_float(PyObject *o)
 NATIVE(route_experts, 11, {
     Call call(a[10]);
     const at::Tensor &x = call.rows(a[0], 2, "logits");
-    const int type = type_of(x, "logits"), T = as_extent(x.size(0), "logits"), E = as_extent(x.size(1), "logits"), k = as_int(a[1]);
+    const int type = type_of(x, "logits"), T = as_extent(x.size(0), "logits"), E = as_extent(x.size(1), "logits"), k = whole(a[1], "k");
     const at::Tensor *bias = a[3] == Py_None ? nullptr : &call.dense(a[3], at::kFloat, {E}, "bias");
-    const int sigmoid = as_bool(a[2]), groups = as_int(a[4]), kept = as_int(a[5]), group_top = as_int(a[6]), renormalise = as_bool(a[7]);
+    const int sigmoid = as_bool(a[2]), groups = whole(a[4], "groups"), kept = whole(a[5], "kept"), group_top = whole(a[6], "group_top"), renormalise = as_bool(a[7]);
     const float factor = as_float(a[8]);
-    if (k < 1) fail(CONV_ERR_INVALID_ARG, "route_experts");
+    if (k < 1 || k > EXPERTS_MOST_CHOICES) fail(CONV_ERR_INVALID_ARG, "route_experts");
     Results out(call, a[9], 2);
     const at::Tensor ids = out.dense({T, k}, at::kInt, x, "ids"), weights = out.dense({T, k}, at::kFloat, x, "weights");
     run("route_experts", lib.route_experts, T, E, k, x.data_ptr(), type, row_distance(x, "logits"), bias ? (const float *)bias->data_ptr() : nullptr, sigmoid, groups, kept, group_top,
@@ -384,9 +396,9 @@ NATIVE(expert_rows, 5, {
     Call call(a[4]);
     const at::Tensor &ids = call.on_device(tensor(a[0], "ids"), "ids");
     if (ids.scalar_type() != at::kInt || !ids.is_contiguous()) refuse(PyExc_TypeError, "ids must be a contiguous int32 tensor");
-    const int pairs = as_extent(ids.numel(), "ids"), E = as_int(a[1]), align = as_int(a[2]);
+    const int pairs = as_extent(ids.numel(), "ids"), E = whole(a[1], "experts"), align = whole(a[2], "align");
     const int R = lib.expert_rows_capacity(pairs, E, align);
-    if (E < 1 || (R == 0 && (pairs > 0 || align != 1))) fail(CONV_ERR_INVALID_ARG, "expert_rows");
+    if (E < 1 || E > EXPERTS_MOST || (R == 0 && (pairs > 0 || align != 1))) fail(CONV_ERR_INVALID_ARG, "expert_rows");
     Results out(call, a[3], 3);
     const at::Tensor offsets = out.dense({E + 1}, at::kInt, ids, "offsets"), rows = out.dense({R}, at::kInt, ids, "rows"),
                      place = out.dense(ids.sizes(), at::kInt, ids, "place");

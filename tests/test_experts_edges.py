@@ -257,3 +257,27 @@ def test_calls_give_up_the_interpreter_lock(stand_in):
     for i, call in enumerate(calls):
         call()
         assert list(stand_in) == [i + 1, 0], i
+
+
+# ---- whole numbers --------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_whole_numbers_that_the_library_cannot_take():
+    """2^32 + 2 is not 2; and counts that are refused are refused before anything of that size is made."""
+    from paper_2104_04731_amd.binding import ConvError
+    x, ids = torch.randn(4, 8, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    off, wrap = torch.zeros(2, dtype=torch.int32, device="cuda"), 2 ** 32
+    q, s = torch.zeros(4, 256, device="cuda").to(E4M3), torch.ones(2, 4, device="cuda")
+    rows = ids[:, 0].contiguous()
+    for bad in (dict(k=wrap + 2), dict(k=-wrap + 2), dict(groups=wrap + 1), dict(kept=wrap + 1), dict(group_top=wrap + 1), dict(k=10 ** 30)):
+        with pytest.raises(ValueError):
+            xp.route_experts(x, **{"k": 2, **bad})
+    for call in (lambda: xp.expert_rows(ids, wrap + 8), lambda: xp.expert_rows(ids, 8, align=wrap + 1), lambda: xp.quantize_fp8(x, rows=rows, per_row=wrap + 1),
+                 lambda: xp.gemm_fp8_experts(q, s, q[None], torch.ones(1, 1, 2, device="cuda"), off, rows=rows, per_row=wrap + 1)):
+        with pytest.raises(ValueError):
+            call()
+    before = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    for call in (lambda: xp.route_experts(torch.zeros(2 ** 16, 8, device="cuda"), 2 ** 14), lambda: xp.expert_rows(ids[:0], 2 ** 31 - 1), lambda: xp.expert_rows(ids[:0], 1025)):
+        with pytest.raises(ConvError):
+            call()
+    assert torch.cuda.max_memory_allocated() - before < 2 ** 24
