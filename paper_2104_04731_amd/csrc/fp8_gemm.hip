@@ -231,8 +231,8 @@ struct Tile {
     static __device__ __forceinline__ int turn_b(int r) { return turn((r & 3) | (r >> 3 & 3) << 2); }
 };
 
-// How whole blocks come into LDS: by transfers past the registers (rows on 16 bytes), through registers (any rows), both with 32-bit offsets within
-// a tile's rows (with rows[]: all of A's); or row by row.
+// How whole blocks come into LDS: by transfers past the registers (rows on 16 bytes), through registers (any rows), both with 32-bit offsets from
+// the tile's first row (with rows[], whose rows may be any: from A's first); or row by row.
 enum Way : int { WAY_ROWS = 0, WAY_REGISTERS = 1, WAY_TRANSFERS = 2 };
 
 // Bound by the matrix units, and those by the power they may take.  bfloat16 results with 8-bit sums: 8192 x 8192, depth 4096, in 279 us one after another (1.97 PFLOP/s;
@@ -301,27 +301,22 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS, TM * TN <= 64 * 64 && (FAST |
     auto live = [&](int i) { return PARTS == 1 || f_lo + i * PARTS + part < f_hi; };
 
     // this wave's transfers: eight rows each, lane / 8, in chunk lane % 8 of the row's place
-    const uint8_t *a_base = p.a, *b_base = p.b + (e_rows + n0) * p.ldb;
-    if constexpr (KIND != GEMM_EXPERTS) a_base += (long long)at.m0 * p.lda;
+    const bool listed = KIND == GEMM_EXPERTS && p.rows;
+    const uint8_t *a_base = listed ? p.a : p.a + (long long)at.m0 * p.lda, *b_base = p.b + (e_rows + n0) * p.ldb;
+    // the tile's row r, and rows past the group's end as one that there is: from a_base on
+    auto a_row_at = [&](int r) { return listed ? max(0, at.m0 + r < at.m_end ? a_row_of<KIND>(p, at.m0 + r) : 0) : min(r, at.m_end - 1 - at.m0); };
     unsigned a_off[L::LOADS_A], b_off[L::LOADS_B], sa_off = 0, sb_off = 0;
 #pragma unroll
     for (int j = 0; j < L::LOADS_A; ++j) {
         const int r = L::a_rows(wave, j) + (lane >> 3);
-        long long row;
-        if constexpr (KIND == GEMM_EXPERTS) row = max(0, at.m0 + r < at.m_end ? a_row_of<KIND>(p, at.m0 + r) : 0);
-        else row = min(r, p.M - 1 - at.m0);
-        a_off[j] = (unsigned)(row * p.lda) + ((lane & 7) ^ L::turn_a(r)) * 16;
+        a_off[j] = (unsigned)(a_row_at(r) * p.lda) + ((lane & 7) ^ L::turn_a(r)) * 16;
     }
 #pragma unroll
     for (int j = 0; j < L::LOADS_B; ++j) {
         const int r = L::b_rows(wave, j) + (lane >> 3);
         b_off[j] = (unsigned)((long long)min(r, p.N - 1 - n0) * p.ldb) + ((lane & 7) ^ L::turn_b(r)) * 16;
     }
-    if (wave < TM / 64) {
-        const int r = wave * 64 + lane;
-        if constexpr (KIND == GEMM_EXPERTS) sa_off = 4u * (unsigned)max(0, at.m0 + r < at.m_end ? a_row_of<KIND>(p, at.m0 + r) : 0);
-        else sa_off = 4u * (unsigned)min(at.m0 + r, p.M - 1);
-    }
+    if (wave < TM / 64) sa_off = 4u * (unsigned)((listed ? 0 : at.m0) + a_row_at(wave * 64 + lane));
     if (BROWS && wave < TN / 64) sb_off = 4u * (unsigned)min(n0 + wave * 64 + lane, p.N - 1);
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)mem;
     constexpr int PIECES = L::LOADS_A + L::LOADS_B + 1;   // the last: scales
@@ -447,10 +442,7 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS, TM * TN <= 64 * 64 && (FAST |
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
                 const int r = row_of(i);
-                long long row;
-                if (i >= CHUNKS_A) row = min(r - TM, p.N - 1 - n0);
-                else if (KIND == GEMM_EXPERTS) row = max(0, at.m0 + r < at.m_end ? a_row_of<KIND>(p, at.m0 + r) : 0);
-                else row = min(r, p.M - 1 - at.m0);
+                const long long row = i >= CHUNKS_A ? min(r - TM, p.N - 1 - n0) : a_row_at(r);
                 off[i] = (unsigned)(row * (i < CHUNKS_A ? p.lda : p.ldb)) + (tid & 7) * 16;
             }
             v4u v[CHUNKS];
@@ -780,7 +772,7 @@ hipError_t launch_few(const Fp8Problem &p, GemmKind kind, hipStream_t st)
 hipError_t launch_fp8_gemm(const Fp8Problem &p, GemmKind kind, hipStream_t st)
 {
     const bool on16 = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | (uintptr_t)p.lda | (uintptr_t)p.ldb) & 15) == 0;
-    const bool near = 256 * p.ldb < 0xffffffffll && (kind == GEMM_EXPERTS ? (long long)p.a_rows : 256) * p.lda < 0xffffffffll;
+    const bool near = 256 * p.ldb < 0xffffffffll && (p.rows ? (long long)p.a_rows : 256) * p.lda < 0xffffffffll;
     const Way way = !near ? WAY_ROWS : on16 ? WAY_TRANSFERS : WAY_REGISTERS;
     const double area = (double)p.M * p.N * (kind == GEMM_GRAD ? p.E : 1);
     const double rows = kind == GEMM_EXPERTS ? (double)p.M / p.E : p.M;   // of a weight matrix, in the mean

@@ -1,4 +1,4 @@
-"""Calls of the experts' entry points beside a stand-in for the launch (launch_recorder.cpp): what each would launch, as JSON.
+"""Calls of the experts' entry points beside a stand-in for the launch (experts_recorder.cpp): what each would launch, as JSON.
 
 argv: the stand-in, the library, a JSON list of [function, arguments]; of the arguments "p" is a pointer on 16 bytes, "odd" one that is not, null none, a list
 [n] a long long, a number with a point a float.  The stand-in is loaded first, so the library's launches go to it; no memory is touched.
@@ -24,5 +24,5 @@ out = []
 for function, arguments in json.loads(sys.argv[3]):
     before = recorded[0]
     rc = getattr(lib, function)(*map(argument, arguments))
-    out.append(dict(rc=rc, launches=recorded[0] - before, workgroups=recorded[1], threads=recorded[2], kernel=name.value.decode()))
+    out.append(dict(rc=rc, launches=recorded[0] - before, workgroups=recorded[1], threads=recorded[2], way=recorded[3], kernel=name.value.decode()))
 print(json.dumps(out))

@@ -18,8 +18,8 @@ E4M3 = torch.float8_e4m3fn
 def launches(tmp_path_factory):
     """What calls of the C entry points would launch (nothing runs)."""
     from paper_2104_04731_amd import build
-    recorder = str(tmp_path_factory.mktemp("host") / "launch_recorder.so")
-    subprocess.run(["g++", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-I/opt/rocm/include", os.path.join(HOST, "launch_recorder.cpp"), "-o", recorder],
+    recorder = str(tmp_path_factory.mktemp("host") / "experts_recorder.so")
+    subprocess.run(["g++", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-I/opt/rocm/include", os.path.join(HOST, "experts_recorder.cpp"), "-o", recorder],
                    check=True, timeout=300)
 
     def run(calls):
@@ -163,6 +163,52 @@ def test_host_quantises_as_many_blocks_as_a_launch_holds(launches):
         assert (got["rc"], got["launches"], got["workgroups"]) == (0, 1, n), (call, got)
     refused = [rows(2 ** 30, 512), rows(2 ** 31 - 1, 1), columns(2 ** 30, 512), columns(2 ** 31 - 1, 1), tiles(1024, 2 ** 20, 2 ** 20), tiles(2 ** 30, 2 ** 30, 2 ** 29)]
     assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(UNSUPPORTED, 0)] * len(refused)
+
+
+ROWS, REGISTERS, TRANSFERS = range(3)   # how operands come into a tile
+
+
+def test_host_experts_rows_past_4_gib(launches):
+    """Operands whose rows follow one another are reached from a tile's first row on, however many rows are before it; through a list all of them have to be within 32 bits."""
+    for fast in (0, 1):
+        long = [experts_call(2 ** 21 + 999, 2 ** 21 + 999, 64, 130, 2048, rows=False, fast=fast), experts_call(2 ** 21 + 999, 2 ** 21 + 999, 64, 4096, 2048, rows=False, fast=fast, on16=False),
+                experts_call(3000, 3000, 8, 130, 2048, lda=2 ** 23, rows=False, fast=fast), experts_call(3000, 3000, 8, 130, 2048, lda=2 ** 23, fast=fast),
+                experts_call(3000, 3000, 8, 130, 2048, lda=2 ** 24, rows=False, fast=fast), experts_call(3000, 3000, 8, 4096, 2048, fast=fast)]
+        assert [(c["rc"], c["way"]) for c in launches(long)] == [(0, w) for w in (TRANSFERS, REGISTERS, TRANSFERS, ROWS, ROWS, TRANSFERS)]
+
+
+def some_rows(g, R, K):
+    """e4m3 of R rows, made on the GPU."""
+    return torch.randint(0, 0x70, (R, K), generator=g, dtype=torch.uint8, device="cuda").view(E4M3)
+
+
+def product_64(a, sa, w, sw):
+    """Rows a [n, K] with scales [blocks, n] times w [N, K] with scales for 128 x 128, and the slack of a sum in 32 bits."""
+    K, n128 = a.shape[1], torch.arange(len(w), device="cuda") // 128
+    av = a.double() * sa.t().repeat_interleave(128, 1)[:, :K].double()
+    wv = w.double() * sw[n128].repeat_interleave(128, 1)[:, :K].double()
+    return av @ wv.t().contiguous(), (K + 8) * 2.0 ** -23 * (av.abs() @ wv.abs().t().contiguous())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("off16", [0, 1])
+@pytest.mark.parametrize("fast", [False, True])
+def test_experts_rows_past_4_gib(off16, fast):
+    """Groups that begin before, at and after the 4 GiB of the left operand; parts of each checked."""
+    g = torch.Generator("cuda").manual_seed(3)
+    R, K, N, E = 2 ** 21 + 1500, 2048, 130, 6
+    a = some_rows(g, R * K // 2048 + 1, 2048).view(-1)[off16:off16 + R * K].view(R, K)
+    sa, w, sw = torch.rand(K // 128, R, generator=g, device="cuda") + 0.5, some_rows(g, E * N, K).view(E, N, K), torch.rand(E, 2, K // 128, generator=g, device="cuda") + 0.5
+    off = [0, 1000, 2 ** 20, 2 ** 21 - 70, 2 ** 21 + 40, 2 ** 21 + 40, 2 ** 21 + 1400]
+    got = xp.gemm_fp8_experts(a, sa, w, sw, torch.tensor(off, dtype=torch.int32, device="cuda"), dtype=torch.float32, fast_sums=fast)
+    for e in range(E):
+        for i in {off[e], max(off[e], off[e + 1] - 90)}:
+            j = min(i + 90, off[e + 1])
+            if j > i:
+                want, slack = product_64(a[i:j], sa[:, i:j], w[e], sw[e])
+                # (fast sums: 2^-9 of a block's largest product a block: of 120 x 120, scales up to 1.5)
+                assert ((got[i:j].double() - want).abs() <= slack + 2.0 ** -24 * want.abs() + (2.0 ** -9 * (120 * 1.5) ** 2 * K // 128 if fast else 0)).all(), (e, i)
+    assert not got[off[-1]:].any()
 
 
 # ---- gradients are calls of their own -----------------------------------------------------------------------------------
