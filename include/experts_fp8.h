@@ -57,8 +57,10 @@ int silu_gate_backward(int rows, int cols, const void *x, long long ldx, const v
 
 /* ---- products ------------------------------------------------------------------------------------------------------
  * C[m][n] = sum over blocks b of 128 of K:  sa[b][m] * sb * (sum over k in b of A[m][k] * B[n][k]), 32-bit sums,
- * rounded once to out_type.  fast_sums != 0: the sum within a block may be taken by the 8-bit matrix instruction, up to twice as fast,
- * which keeps products to 2^-17 of the block's largest or so (1.5e-5 of a result in the mean: a hundredth of rounding to bfloat16).  A [M][K], sa [ceil(K/128)][M] dense.  b_rows == 0: sb[n / 128][b] ([ceil(N/128)][ceil(K/128)],
+ * rounded once to out_type.  fast_sums != 0: the sum within a block may be taken by the 8-bit matrix instruction, up to twice as fast, which
+ * cuts each of eight neighbouring products (k = 8 i ... 8 i + 7) towards zero to a multiple of 2^-13 of the largest one's power of two: a result is then up to
+ * 7 * 2^-13 (8.5e-4) of the sum of its terms' magnitudes off, more than rounding to float16; with values of one size and random sign 1.5e-5 of the result in the mean, a
+ * hundredth of rounding to bfloat16, but losses of terms of one sign add up.  A [M][K], sa [ceil(K/128)][M] dense.  b_rows == 0: sb[n / 128][b] ([ceil(N/128)][ceil(K/128)],
  * weights); != 0: sb[b][n] ([ceil(K/128)][N]).  Scales are any f32.  Gradients are the same product: of the input with the
  * weights quantised transposed, of the weights with both operands quantised by columns. */
 int gemm_fp8_nt(int M, int N, int K, const uint8_t *A, long long lda, const float *sa, const uint8_t *B, long long ldb, const float *sb, int b_rows,

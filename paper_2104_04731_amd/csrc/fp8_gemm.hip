@@ -4,9 +4,10 @@
 // A block's sum starts from zero in the matrix units and is scaled and added to 32-bit sums by the vector unit: four fused multiply-adds a
 // lane to 16 x 16 results.  B's rows are the instruction's rows and A's its columns: a lane's results then belong to one row m, whose
 // scale is one number a lane and a block, and to neighbouring columns n, which leave in 16-byte stores.
-// How a block is summed: the 8-bit instructions (v_mfma_f32_16x16x128_f8f6f4, and the 32-deep one alike) align the products they add
-// to the largest and drop what lies below: 448 * 448 + 1 gives 448 * 448, and sums of 128 normal values are 1.5e-5 off in the mean, up to 3.4e-4 of the
-// largest product (measured).  That is a hundredth of what rounding to bfloat16 costs but not a 32-bit sum, so it is the caller's
+// How a block is summed: the 8-bit instruction (v_mfma_f32_16x16x128_f8f6f4) aligns each eight neighbouring products to the largest of them and cuts
+// the others towards zero 13 bits below its power of two: beside 256 * 256 a 7.5 is lost and a 15 becomes 8, in the next eight a 0.0625 is kept (measured).  So a
+// result is up to 7 * 2^-13 of the sum of its terms' magnitudes off, and always towards zero; sums of 128 normal values 1.5e-5 in the mean.  That is a
+// hundredth of what rounding to bfloat16 costs but not a 32-bit sum, so it is the caller's
 // choice (FAST); without it the values are widened to bfloat16, exactly, for v_mfma_f32_16x16x32_bf16, whose sums are 32-bit ones (8.5e-9), at half the rate.
 // Two kernels: tiles through LDS, bound by the matrix units; and, for few rows of not too large weights, one that streams B from memory into
 // registers with the depth shared among the waves of a workgroup, bound by B's bytes or the latency of one round of loads.

@@ -60,8 +60,9 @@ def silu_gate_backward(x: torch.Tensor, dh: torch.Tensor, out=None, stream=None)
 
 def gemm_fp8_nt(a, a_scale, b, b_scale, b_rows=False, dtype=torch.bfloat16, fast_sums=False, out=None, stream=None):
     """a [M, K] times b [N, K] transposed -> [M, N].  a_scale [ceil(K/128), M]; b_scale [ceil(N/128), ceil(K/128)], with
-    b_rows [ceil(K/128), N].  fast_sums: a block's 128 products may be summed by the 8-bit matrix instruction, up to twice as fast
-    and 1.5e-5 off in the mean (a hundredth of rounding to bfloat16); else in 32 bits throughout."""
+    b_rows [ceil(K/128), N].  fast_sums: a block's 128 products may be summed by the 8-bit matrix instruction, up to twice as fast, which
+    cuts each of eight neighbouring products towards zero to a multiple of 2^-13 of the largest one's power of two: off by up to 8.5e-4 of the sum of the terms'
+    magnitudes, in the mean of values of one size 1.5e-5 of the result (a hundredth of rounding to bfloat16); else in 32 bits throughout."""
     return (_native or _calls()).gemm_fp8_nt(a, a_scale, b, b_scale, b_rows, dtype, fast_sums, out, stream)
 
 

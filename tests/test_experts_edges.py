@@ -177,8 +177,11 @@ def test_host_experts_rows_past_4_gib(launches):
         assert [(c["rc"], c["way"]) for c in launches(long)] == [(0, w) for w in (TRANSFERS, REGISTERS, TRANSFERS, ROWS, ROWS, TRANSFERS)]
 
 
+CUT = 7 * 2.0 ** -13   # fast sums: of eight neighbouring products all but the largest lose less than 2^-13 of it
+
+
 def some_rows(g, R, K):
-    """e4m3 of R rows, made on the GPU."""
+    """e4m3 of R rows, none negative, made on the GPU."""
     return torch.randint(0, 0x70, (R, K), generator=g, dtype=torch.uint8, device="cuda").view(E4M3)
 
 
@@ -206,9 +209,45 @@ def test_experts_rows_past_4_gib(off16, fast):
             j = min(i + 90, off[e + 1])
             if j > i:
                 want, slack = product_64(a[i:j], sa[:, i:j], w[e], sw[e])
-                # (fast sums: 2^-9 of a block's largest product a block: of 120 x 120, scales up to 1.5)
-                assert ((got[i:j].double() - want).abs() <= slack + 2.0 ** -24 * want.abs() + (2.0 ** -9 * (120 * 1.5) ** 2 * K // 128 if fast else 0)).all(), (e, i)
+                assert ((got[i:j].double() - want).abs() <= slack + 2.0 ** -24 * want.abs() + (CUT * want if fast else 0)).all(), (e, i)
     assert not got[off[-1]:].any()
+
+
+# ---- fast sums ------------------------------------------------------------------------------------------------------------
+def one_signed(g, rows, K, worst, left):
+    """e4m3 values, none negative: a 256 in every eight of a row beside values just below what is kept (7.5 * 1 of 256 * 256 / 2^13 = 8), or magnitudes over many binades."""
+    if worst:
+        v = torch.full((rows, K), 7.5 if left else 1.0, device="cuda")
+        v[:, 3::8] = 256.0
+    else:
+        v = torch.exp2(16 * torch.rand(rows, K, generator=g, device="cuda") - 8) * (1 + torch.rand(rows, K, generator=g, device="cuda"))
+    out = torch.zeros(rows, -(-K // 16) * 16, dtype=torch.uint8, device="cuda")[:, :K].view(E4M3)
+    out.view(torch.uint8).copy_(v.clamp(max=448).to(E4M3).view(torch.uint8))
+    return out
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("worst", [True, False])
+@pytest.mark.parametrize("fast", [True, False])
+@pytest.mark.parametrize("size", [(65, 129, 384), (300, 520, 2048), (2900, 3000, 640), (4000, 4104, 1100)])
+def test_sums_of_one_sign(size, fast, worst):
+    """Every term's loss in one direction, in each tile and four parts: within the bound of fast sums, and in 32 bits within theirs."""
+    M, N, K = size
+    g = torch.Generator("cuda").manual_seed(M)
+    a, b = one_signed(g, M, K, worst, True), one_signed(g, N, K, worst, False)
+    sa, sw = torch.ones(-(-K // 128), M, device="cuda"), torch.ones(-(-N // 128), -(-K // 128), device="cuda")
+    m = torch.cat([torch.arange(0, M, 61), torch.arange(M - 9, M)]).cuda()
+    got = [xp.gemm_fp8_nt(a, sa, b, sw, dtype=torch.float32, fast_sums=fast)[m]]
+    got.append(xp.gemm_fp8_nt(a, sa, b, torch.ones(-(-K // 128), N, device="cuda"), b_rows=True, dtype=torch.float32, fast_sums=fast)[m])
+    off = torch.tensor([0, M // 3, M], dtype=torch.int32, device="cuda")
+    w = torch.empty(2, N, b.stride(0), dtype=torch.uint8, device="cuda")[..., :K].view(E4M3)
+    w.view(torch.uint8).copy_(b.view(torch.uint8)[None].expand(2, N, K))
+    got.append(xp.gemm_fp8_experts(a, sa, w, torch.stack([sw, sw]), off, dtype=torch.float32, fast_sums=fast)[m])
+    one = torch.tensor([0, K], dtype=torch.int32, device="cuda")
+    got.append(xp.gemm_fp8_experts_grad(a, sa, b, torch.ones(-(-K // 128), N, device="cuda"), one, fast_sums=fast)[0][m])
+    want = a[m].double() @ b.double().t().contiguous()
+    for i, v in enumerate(got):
+        assert ((v.double() - want).abs() <= ((CUT if fast else 0) + (K + 8) * 2.0 ** -23) * want).all(), i
 
 
 # ---- gradients are calls of their own -----------------------------------------------------------------------------------
