@@ -11,7 +11,7 @@
 #include "../../include/experts_fp8.h"
 
 extern PyMethodDef experts_methods[];
-bool experts_library(void *handle);
+void experts_library(void *handle);
 
 namespace {
 
@@ -26,6 +26,7 @@ struct Library {
     LIBRARY_CALLS(CALL)
 #undef CALL
 } lib;
+const char *missing = nullptr;   // one that the loaded library has not got (a library from before these calls)
 
 template <class... A>
 [[noreturn]] void refuse(PyObject *error, const char *format, A... a)
@@ -76,9 +77,14 @@ int whole(PyObject *o, const char *what)
 
 // The call's device (the first tensor's, which must be the current one) and stream.  Results are allocated for the stream that the call runs on.
 struct Call {
-    int device = -1;
+    int device;
     c10::hip::HIPStream stream;
-    explicit Call(PyObject *s) : stream(c10::hip::getCurrentHIPStream())
+    static int none_yet()
+    {
+        if (missing) refuse(PyExc_RuntimeError, "the loaded library has no symbol %s", missing);
+        return -1;
+    }
+    explicit Call(PyObject *s) : device(none_yet()), stream(c10::hip::getCurrentHIPStream())
     {
         if (s == Py_None) return;
         PyObject *id = PyObject_GetAttrString(s, "stream_id"), *index = id ? PyObject_GetAttrString(s, "device_index") : nullptr;
@@ -445,18 +451,13 @@ NATIVE(combine_experts_backward, 7, {
 
 }  // namespace
 
-bool experts_library(void *handle)
+void experts_library(void *handle)
 {
-    Library found;
-#define CALL(name)                                                                           \
-    if (!(found.name = reinterpret_cast<decltype(&::name)>(dlsym(handle, #name)))) {        \
-        PyErr_SetString(PyExc_RuntimeError, "the loaded library has no symbol " #name);       \
-        return false;                                                                         \
-    }
+    missing = nullptr;
+#define CALL(name) \
+    if (!(lib.name = reinterpret_cast<decltype(&::name)>(dlsym(handle, #name)))) missing = #name;
     LIBRARY_CALLS(CALL)
 #undef CALL
-    lib = found;
-    return true;
 }
 
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, nullptr}

@@ -366,3 +366,29 @@ def test_whole_numbers_that_the_library_cannot_take():
         with pytest.raises(ConvError):
             call()
     assert torch.cuda.max_memory_allocated() - before < 2 ** 24
+
+
+# ---- a library without these calls ------------------------------------------------------------------------------------------
+def test_a_library_without_the_experts_calls_keeps_the_others(tmp_path, lib):
+    """The binding takes a library that was built before them (in a process of its own: the library is replaced): its calls work, the missing ones say what they miss."""
+    from paper_2104_04731_amd import build
+    if not os.path.exists(build.NATIVE):
+        pytest.fail("not built")
+    source = tmp_path / "older.cpp"
+    source.write_text('extern "C" {\n' + "".join(f"int {n}() {{ return 0; }}\n" for n in lib.EXPORTS) + "}\n")
+    subprocess.run(["g++", "-shared", "-fPIC", str(source), "-o", str(tmp_path / "older.so")], check=True, timeout=120)
+    code = f"""
+import ctypes, sys
+sys.path.insert(0, {ROOT!r})
+import torch
+from paper_2104_04731_amd import _native
+_native.set_error_class(RuntimeError)
+_native.set_library(ctypes.CDLL({str(tmp_path / 'older.so')!r})._handle)
+try:
+    _native.route_experts(torch.zeros(1, 4), 1, False, None, 1, 1, 1, True, 1.0, None, None)
+except RuntimeError as e:
+    assert "no symbol" in str(e), e
+    print("ok")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stderr[-2000:]
