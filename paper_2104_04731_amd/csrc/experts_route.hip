@@ -509,9 +509,16 @@ hipError_t launch_route_backward(const RouteProblem &p, hipStream_t st)
 
 hipError_t launch_expert_rows(const OrderProblem &p, hipStream_t st)
 {
-    // From how many pairs on counting once, in three launches, takes less time than counting all of them in every workgroup, us (131072 pairs of 64 experts: 11.5 | 17.8,
-    // of 256 16.2 | 16.5, of 1000 38.9 | 19.8; 2^20 24 | 123, 32 | 113, 58 | 123; 65536 of 256 13.5 | 9.8).
-    const int many = p.E <= 256 ? 1 << 16 : 3 << 17;
+    // From how many pairs on counting once, in three launches, takes less time than counting all of them in every workgroup: the three begin at 10 us and grow with the
+    // experts' number, the one grows with the pairs'.  us, one | three (random ids, one call after another in a graph; 2^20 pairs of 64, 256 and 1000 experts 123 | 24,
+    // 113 | 32, 123 | 58):
+    //   pairs     64 experts   128          256          384          512          1024
+    //    65536   10.0 | 10.5    9.6 | 10.8   9.5 | 11.1   9.9 | 13.5  10.3 | 13.5  11.9 | 18.9
+    //    81920   12.9 | 10.6   12.6 | 10.8  12.2 | 13.0  12.7 | 15.5  13.1 | 15.8  15.4 | 21.7
+    //   131072   17.7 | 10.7   16.9 | 11.1  16.1 | 13.6  16.5 | 18.4  16.8 | 18.6  18.8 | 29.0
+    //   163840   22.2 | 12.2   21.2 | 12.7  20.2 | 14.9  20.5 | 17.8  20.8 | 18.1  23.1 | 24.2
+    //   262144   32.8 | 12.5   31.1 | 13.2  29.1 | 15.8  29.5 | 20.8  30.2 | 21.1  33.2 | 31.7
+    const int many = p.E <= 128 ? 1 << 16 : 49152 + 192 * p.E;
     int bits = 0;
     while ((1 << bits) < p.E) ++bits;
     const auto lds = [&](int waves) { return 4u * ((3 * p.E + 4) / 4 * 4) + 2u * waves * p.E; };

@@ -392,3 +392,34 @@ except RuntimeError as e:
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stderr[-2000:]
+
+
+# ---- which way the order of rows goes -----------------------------------------------------------------------------------------
+def rows_call(pairs, E, align=1):
+    return ["expert_rows", [pairs, E, align, "p", "p", "p", "p", None]]
+
+
+def test_host_order_of_rows_takes_the_faster_way(launches):
+    """One launch or three, at numbers of pairs where one of the two is faster by a tenth and more (us: 16.1 | 13.6, 29.5 | 20.8, 46.9 | 23.1; 9.5 | 11.1, 12.7 | 15.5, 18.8 | 29.0)."""
+    three = [(131072, 256), (262144, 384), (393216, 384), (163840, 512), (393216, 1024), (81920, 8), (81920, 128), (98304, 192)]
+    one = [(65536, 256), (81920, 384), (131072, 1024), (131072, 512), (65536, 128), (32768, 64), (1, 1), (0, 5)]
+    got = launches([rows_call(*c) for c in three + one])
+    assert [(c["rc"], c["launches"]) for c in got] == [(0, 3)] * len(three) + [(0, 1)] * len(one)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pairs,E", [(90112, 192), (98304, 256), (98305, 256), (147456, 512), (147457, 512), (245760, 1024), (245761, 1024)])
+def test_order_of_rows_around_the_change_of_ways(pairs, E):
+    g = torch.Generator("cuda").manual_seed(E)
+    ids = torch.randint(-1, E + 1, (pairs,), generator=g, dtype=torch.int32, device="cuda")
+    ids[pairs // 3:pairs // 2] = E - 1
+    off, rows, place = xp.expert_rows(ids, E, align=16)
+    key = torch.where((ids >= 0) & (ids < E), ids, E).long()
+    counts = torch.bincount(key, minlength=E + 1)[:E]
+    starts = torch.cat([counts.new_zeros(1), ((counts + 15) // 16 * 16).cumsum(0)])
+    assert torch.equal(off.long(), starts)
+    order = torch.sort(key, stable=True).indices[:int(counts.sum())]
+    at = starts[key[order]] + torch.arange(len(order), device="cuda") - (counts.cumsum(0) - counts)[key[order]]
+    want_rows, want_place = torch.full_like(rows, -1), torch.full_like(place, -1)
+    want_rows[at], want_place[order] = order.int(), at.int()
+    assert torch.equal(rows, want_rows) and torch.equal(place, want_place)
