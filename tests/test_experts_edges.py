@@ -423,3 +423,167 @@ def test_order_of_rows_around_the_change_of_ways(pairs, E):
     want_rows, want_place = torch.full_like(rows, -1), torch.full_like(place, -1)
     want_rows[at], want_place[order] = order.int(), at.int()
     assert torch.equal(rows, want_rows) and torch.equal(place, want_place)
+
+
+# ---- every kernel of the products -----------------------------------------------------------------------------------------------
+DENSE, EXPERTS, GRAD = range(3)
+FAR = 2 ** 24   # a distance of rows at which a tile's are not within 32 bits
+# (M, N, depth), with experts their rows and the list's source rows; what takes a tile of 256, 128, 64, 64 in four parts, and the kernel for few rows with the depth in 1, 4, 8
+SIZES = {
+    (256, 1): dict(dense=(3900, 4104, 1100), experts=((1700, 0, 2296), 4104, 1100), grad=((700, 0, 901), 2300, 2200)),
+    (128, 1): dict(dense=(2900, 3000, 650), experts=((900, 2, 0, 1598), 2600, 650), grad=((300, 0, 900, 901), 1100, 2050)),
+    (64, 1): dict(dense=(257, 300, 390), experts=((70, 0, 230), 300, 390), grad=((300, 0, 389), 130, 200)),
+    (64, 4): dict(dense=(300, 520, 2000), experts=((70, 3, 227), 520, 2000), grad=((1605, 1695), 130, 200)),
+}
+FEW = {(mt, split): dict(dense=(rows, 300, depth), experts=(counts, 140, depth))
+       for mt, rows, counts in ((1, 7, (9, 0, 17, 3)), (2, 20, (41, 0, 30, 33))) for split, depth in ((1, 200), (4, 400), (8, 1300))}
+
+
+def all_cases():
+    """(what takes it, kind, b_rows, fast, how the rows lie, sizes)"""
+    out = []
+    for (tile, parts), sizes in SIZES.items():
+        for kind, b_rows in ((DENSE, 0), (DENSE, 1), (EXPERTS, 0), (GRAD, 1)):
+            size = sizes[("dense", "experts", "grad")[kind]]
+            for fast in (0, 1):
+                if tile == 256:
+                    out += [((tile, parts), kind, b_rows, 1, TRANSFERS, size)] if fast else []
+                    continue
+                out += [((tile, parts), kind, b_rows, fast, way, size) for way in (TRANSFERS, REGISTERS)]
+                if tile == 128 and kind != EXPERTS:   # (few columns, whose rows lie far apart, and many rows)
+                    size = (120000, 70, 650) if kind == DENSE else ((300, 0, 900, 901), 30000, 70)
+                out.append(((tile, parts), kind, b_rows, fast, ROWS, size))
+    for (mt, split), sizes in FEW.items():
+        for kind, b_rows in ((DENSE, 0), (DENSE, 1), (EXPERTS, 0)):
+            out += [((mt, split), kind, b_rows, 0, way, sizes[("dense", "experts")[kind]]) for way in (TRANSFERS, REGISTERS)]
+    return out
+
+
+CASES = all_cases()
+
+
+def case_id(c):
+    (a, b), kind, b_rows, fast, way, size = c
+    return f"{'tile' if a > 2 else 'few'}{a}x{b}-{('dense', 'experts', 'grad')[kind]}{'-rows' * b_rows}{'-fast' * fast}-{('far', 'off16', 'on16')[way]}"
+
+
+def distances(case):
+    """(of A's rows, of B's): whole 16 bytes, off them, or too far apart (of experts A's, of which the list reads 260; of weight gradients and dense products B's)."""
+    _, kind, _, _, way, size = case
+    K = sum(size[0]) + 11 if kind == GRAD else size[2]
+    near = -(-K // 16) * 16 + (3 if way == REGISTERS else 0)
+    return (FAR if way == ROWS and kind == EXPERTS else near), (FAR if way == ROWS and kind != EXPERTS else near)
+
+
+def test_host_the_cases_take_every_kernel_of_the_products(launches):
+    """Each case below the kernel that it is for, with its rows brought in as it says; all that the dispatch can launch among them."""
+    import re
+    calls = []
+    for case in CASES:
+        _, kind, b_rows, fast, way, size = case
+        (lda, ldb), on16 = distances(case), way != REGISTERS
+        if kind == DENSE:
+            calls.append(dense_call(*size, b_rows=b_rows, fast=fast, on16=on16, lda=lda, ldb=ldb))
+        elif kind == EXPERTS:
+            counts, N, K = size
+            calls.append(["gemm_fp8_experts", [sum(counts) + 9, 260, len(counts), N, K, "p", [lda], "p", "p", [ldb], "p", "p", "p", 2, "p", [N], 0, fast, None]])
+        else:
+            counts, N, K = size
+            calls.append(["gemm_fp8_experts_grad", [sum(counts) + 11, len(counts), N, K, "p", [lda], "p", "p", [ldb], "p", "p", "p", [K], 0, fast, None]])
+    seen = set()
+    for case, got in zip(CASES, launches(calls)):
+        (a, b), kind, b_rows, fast, way, _ = case
+        name = got["kernel"]
+        tile = re.search(r"fp8_tile_kernelILi(\d+)ELi(\d+)ELi\d+ELi\d+ELi(\d+)EL\w*GemmKindE(\d)ELb([01])ELb([01])E", name)
+        few = re.search(r"fp8_few_kernelILi(\d+)ELi(\d+)EL\w*GemmKindE(\d)ELb([01])E", name)
+        if a > 2:
+            assert tile and tuple(map(int, tile.groups())) == (a, a, b, kind, b_rows, fast) and got["way"] == way, (case, got)
+        else:
+            assert few and tuple(map(int, few.groups())) == (a, b, kind, b_rows), (case, got)
+        seen.add(name)
+    assert len(seen) == 28 + 18
+
+
+def far_apart(v, distance, off16):
+    """The rows of v [.., n, K] (bytes) `distance` apart, beginning off 16 bytes if so asked; what lies between them is NaN as far as 200 bytes behind a row."""
+    n, K = v.numel() // v.shape[-1], v.shape[-1]
+    base = torch.empty(n * distance + 256, dtype=torch.uint8, device="cuda")
+    lead = 5 if off16 else 0
+    rows = base[lead:lead + n * distance].view(n, distance)
+    rows[:, :min(distance, K + 200)] = 0x7f
+    rows[:, :K] = v.view(n, K)
+    return rows[:, :K].view(E4M3).view(*v.shape[:-1], K) if v.dim() == 2 else rows.view(*v.shape[:-1], distance)[..., :K].view(E4M3)
+
+
+def e4m3_bytes(g, *shape):
+    v = torch.randint(0, 256, shape, generator=g, dtype=torch.uint8, device="cuda")
+    return torch.where((v & 0x7f) == 0x7f, v ^ 0x20, v)   # (no NaN)
+
+
+def scaled(v, s):
+    """Rows [n, K] of bytes and their scales [blocks, n] in 64 bits."""
+    return v.contiguous().view(E4M3).double() * s.t().repeat_interleave(128, 1)[:, :v.shape[1]].double()
+
+
+def check_product(got, a, b, fast, what):
+    want, terms = a @ b.t().contiguous(), a.abs() @ b.abs().t().contiguous()
+    slack = ((CUT if fast else 0) + (a.shape[1] + 8) * 2.0 ** -23) * terms + 2.0 ** -24 * want.abs()
+    assert ((got.double() - want).abs() <= slack).all(), what
+
+
+def some(n, step):
+    """Indices of n: every `step`-th, the first and last ones, and both sides of each multiple of 64 up to 300."""
+    near = [torch.arange(max(0, c - 2), min(n, c + 2)) for c in (0, 64, 128, 192, 256, n) if c <= n]
+    return torch.unique(torch.cat([torch.arange(0, n, step), *near])).cuda()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", CASES, ids=case_id)
+def test_every_kernel_of_the_products(case):
+    """Values of each kernel a product can take, rows on and off 16 bytes and 2^24 bytes apart, offsets that cut blocks, gaps in lists; NaN behind every row."""
+    what, kind, b_rows, fast, way, size = case
+    (lda, ldb), off16 = distances(case), way == REGISTERS
+    g = torch.Generator("cuda").manual_seed(sum(what) + 8 * kind)
+    scales = lambda *shape: torch.exp(torch.randn(*shape, generator=g, device="cuda"))  # noqa: E731
+    up = lambda n: -(-n // 128)  # noqa: E731
+    if kind == DENSE:
+        M, N, K = size
+        a, b, sa = e4m3_bytes(g, M, K), e4m3_bytes(g, N, K), scales(up(K), M)
+        sb = scales(up(K), N) if b_rows else scales(up(N), up(K))
+        got = xp.gemm_fp8_nt(far_apart(a, lda, off16), sa, far_apart(b, ldb, off16), sb, b_rows=bool(b_rows), dtype=torch.float32, fast_sums=bool(fast))
+        m, n = some(M, max(1, M // 60)), some(N, max(1, N // 60))
+        of_b = sb[:, n] if b_rows else sb[n // 128].t()
+        check_product(got[m][:, n], scaled(a[m], sa[:, m]), scaled(b[n], of_b), fast, case)
+    elif kind == EXPERTS:
+        counts, N, K = size
+        E, R, rows_of_a = len(counts), sum(counts) + 9, 260
+        a, w, sa, sw = e4m3_bytes(g, rows_of_a, K), e4m3_bytes(g, E, N, K), scales(up(K), rows_of_a), scales(E, up(N), up(K))
+        rows = torch.randint(-9, 2 * rows_of_a + 9, (R,), generator=g, dtype=torch.int32, device="cuda")
+        off = torch.tensor([0, *counts]).cumsum(0)
+        out = torch.full((R, N), float("nan"), device="cuda")
+        got = xp.gemm_fp8_experts(far_apart(a, lda, off16), sa, far_apart(w, ldb, off16), sw, off.int().cuda(), rows=rows, per_row=2, dtype=torch.float32, fast_sums=bool(fast), out=out)
+        n = some(N, max(1, N // 60))
+        for e in range(E):
+            i, j = int(off[e]), int(off[e + 1])
+            if i == j:
+                continue
+            r = i + some(j - i, max(1, (j - i) // 40))
+            is_row = (rows[r] >= 0) & (rows[r] < 2 * rows_of_a)
+            at = (rows[r].long() // 2).clamp(0, rows_of_a - 1)
+            left = torch.where(is_row[:, None], scaled(a[at], sa[:, at]), 0.0)
+            check_product(got[r][:, n], left, scaled(w[e][n], sw[e][n // 128].t()), fast, (case, e))
+        gone = (rows < 0) | (rows >= 2 * rows_of_a)
+        gone[int(off[-1]):] = True
+        assert not got[gone].any() and not got.isnan().any()
+    else:
+        counts, N, K = size
+        E, R = len(counts), sum(counts) + 11
+        a, b, sa, sb = e4m3_bytes(g, N, R), e4m3_bytes(g, K, R), scales(up(R), N), scales(up(R), K)
+        off = torch.tensor([0, *counts]).cumsum(0)
+        got = xp.gemm_fp8_experts_grad(far_apart(a, lda, off16), sa, far_apart(b, ldb, off16), sb, off.int().cuda(), fast_sums=bool(fast))
+        n, k = some(N, max(1, N // 50)), some(K, max(1, K // 50))
+        left, right = scaled(a[n], sa[:, n]), scaled(b[k], sb[:, k])
+        for e in range(E):
+            i, j = int(off[e]), int(off[e + 1])
+            check_product(got[e][n][:, k], left[:, i:j], right[:, i:j], fast, (case, e))
+        assert not got.isnan().any()
