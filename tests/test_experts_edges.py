@@ -587,3 +587,85 @@ def test_every_kernel_of_the_products(case):
             i, j = int(off[e]), int(off[e + 1])
             check_product(got[e][n][:, k], left[:, i:j], right[:, i:j], fast, (case, e))
         assert not got.isnan().any()
+
+
+# ---- quantisation -----------------------------------------------------------------------------------------------------------------
+def e4m3_of(x, scale):
+    """rne_e4m3(clamp(x / scale)) in 64 bits, a NaN where x is one: the nearest of the type's numbers, of two as near the even one."""
+    q = (x.double() / scale).clamp(-448, 448)
+    e = torch.floor(torch.log2(q.abs().clamp(min=2.0 ** -6)))
+    e = torch.where(torch.exp2(e + 1) <= q.abs(), e + 1, torch.where(torch.exp2(e) > q.abs().clamp(min=2.0 ** -6), e - 1, e))
+    step = torch.exp2(e - 3)
+    return (torch.round(q / step) * step).float()   # (round: to even)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["rows", "columns", "tiles"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_quantize_every_16_bit_pattern(dtype, form):
+    """All 65536 numbers of each type that are no larger than 448 scales, at scales over the type's whole range: 127 of them to a block beside the number that sets its scale."""
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(dtype).cuda()
+    x = torch.cat([x, x.new_zeros(-len(x) % 127)]).view(-1, 127)
+    exponents = [-126, -125, -90, -62, -30, -9, -1, 0, 1, 7, 31, 64, 100, 119] if dtype == torch.bfloat16 else list(range(-33, 8, 4)) + [7]
+    for e in exponents:
+        top = 448.0 * 2.0 ** e
+        lead = torch.full((len(x), 1), top, dtype=torch.float64, device="cuda").to(dtype)
+        assert (lead.double() == top).all() or dtype == torch.float16   # (float16: its least numbers are no multiples of 448 scales)
+        fits = torch.where((x.double().abs() <= top) | x.isnan(), x, torch.zeros_like(x))
+        block = torch.cat([lead, fits], 1)
+        scale = torch.exp2(torch.ceil(torch.log2(lead.double() / 448)).clamp(min=-126))
+        want = e4m3_of(block, scale)
+        if form == "rows":
+            q, s = xp.quantize_fp8(block)
+            assert torch.equal(s[0].double(), scale[:, 0])
+        elif form == "columns":
+            q, s = xp.quantize_fp8(block.t().contiguous(), form="columns")
+            assert torch.equal(s[0].double(), scale[:, 0])
+        else:
+            full = torch.zeros(-(-len(block) // 128) * 128, 128, dtype=dtype, device="cuda")
+            full[:len(block)] = block
+            q, s = xp.quantize_fp8(full, form="tiles")
+            assert (s.double() == scale[0, 0]).all()
+            q = q[:len(block)]
+        got = q.float()
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(), want.nan_to_num()), e
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,per_row", [(700, 1032, 4), (4100, 264, 1), (300, 130, 3)])
+def test_quantize_through_a_long_list(rows, cols, per_row, dtype, gate):
+    """The same as of the rows laid out one after another, zeros for those that are none, in every form that takes a list."""
+    g = torch.Generator("cuda").manual_seed(rows)
+    x = torch.randn(rows // 3, cols * (1 + gate), generator=g, device="cuda").to(dtype)
+    take = torch.randint(-20, len(x) * per_row + 20, (rows,), generator=g, dtype=torch.int32, device="cuda")
+    there = (take >= 0) & (take < len(x) * per_row)
+    laid = torch.where(there[:, None], x[(take.long() // per_row).clamp(0, len(x) - 1)], torch.zeros_like(x[:1]))
+    for form in ("rows", "columns", "rows+columns"):
+        for a, b in zip(xp.quantize_fp8(x, form=form, gate=gate, rows=take, per_row=per_row), xp.quantize_fp8(laid, form=form, gate=gate)):
+            assert torch.equal(a.view(torch.uint8) if a.dtype == E4M3 else a, b.view(torch.uint8) if b.dtype == E4M3 else b), form
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("size,apart", [((517, 2056), 0), ((2049, 1000), 24), ((300, 333), 7), ((1, 4096), 0)])
+def test_gate_backward_of_many_rows(size, apart, dtype):
+    """Rows of whole pieces of 16 bytes and others, one after another and apart."""
+    g = torch.Generator("cuda").manual_seed(size[0])
+    rows, cols = size
+
+    def lie(n):
+        return torch.randn(rows, n + apart, generator=g, device="cuda").to(dtype)[:, :n]
+    x, dh = lie(2 * cols), lie(cols)
+    gate, up, d = *x.double().chunk(2, 1), dh.double()
+    s = torch.sigmoid(gate)
+    want = torch.cat([d * up * s * (1 + gate * (1 - s)), d * gate * s], 1)
+    frame = torch.full((rows, 2 * cols + apart), 7.0, dtype=dtype, device="cuda")
+    xp.silu_gate_backward(x, dh, out=frame[:, :2 * cols])
+    # factors of size 1 to (1 + |gate|) and |up|, each of a few roundings in 32 bits
+    slack = 32 * 2.0 ** -23 * d.abs().repeat(1, 2) * torch.cat([(1 + gate.abs()) * up.abs(), gate.abs()], 1)
+    step = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}[dtype]
+    tiny = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}[dtype]
+    assert ((frame[:, :2 * cols].double() - want).abs() <= slack + step * want.abs() + tiny).all()
+    assert (frame[:, 2 * cols:] == 7).all()
