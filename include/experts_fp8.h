@@ -67,8 +67,8 @@ int gemm_fp8_nt(int M, int N, int K, const uint8_t *A, long long lda, const floa
                 void *C, long long ldc, int out_type, int fast_sums, void *stream);
 /* A weight matrix for each expert.  Row r of C, offsets[e] <= r < offsets[e + 1], is the product of A's row r -- with rows
  * (int32 [R]) of A's row rows[r] / per_row -- and W + e * N * ldw (scales at sw + e * ceil(N/128) * ceil(K/128)).  Rows that
- * belong to no expert, and those whose rows[r] is negative or past a_rows * per_row, are zeros.  offsets: int32 [E + 1], rising
- * from 0 to R at most.  A [a_rows][K] (a_rows = R without rows), sa [ceil(K/128)][a_rows]; E up to EXPERTS_MOST. */
+ * belong to no expert (ahead of offsets[0], from offsets[E] on), and those whose rows[r] is negative or past a_rows * per_row, are zeros.  offsets: int32
+ * [E + 1], rising, within 0 to R.  A [a_rows][K] (a_rows = R without rows), sa [ceil(K/128)][a_rows]; E up to EXPERTS_MOST. */
 int gemm_fp8_experts(int R, int a_rows, int E, int N, int K, const uint8_t *A, long long lda, const float *sa, const uint8_t *W, long long ldw,
                      const float *sw, const int32_t *offsets, const int32_t *rows, int per_row, void *C, long long ldc, int out_type, int fast_sums, void *stream);
 /* Their weights' gradients: C[e][n][k] = sum over r in [offsets[e], offsets[e + 1]) of A[n][r] * B[k][r], with A [N][R], sa

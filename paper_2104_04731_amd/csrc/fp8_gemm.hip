@@ -61,6 +61,13 @@ __device__ __forceinline__ Place place_of(const int32_t *offsets, int E, int R, 
     }
 }
 
+// The rows of no expert, counted: those ahead of the first expert's, then those behind the last one's (of a place that is `zeros`).
+struct NoRows {
+    int ahead, behind, count;
+    __device__ __forceinline__ NoRows(const Fp8Problem &p, const Place &at) : ahead(min(max(p.offsets[0], 0), p.M)), behind(at.m0), count(ahead + at.m_end - at.m0) {}
+    __device__ __forceinline__ int operator[](int i) const { return i < ahead ? i : behind + i - ahead; }
+};
+
 __device__ __forceinline__ int xcd_contiguous(int id, int n)
 {
     const int x = id & 7, q = n >> 3, rem = n & 7;
@@ -270,8 +277,9 @@ __global__ __launch_bounds__(64 * WM * WN * PARTS, TM * TN <= 64 * 64 && (FAST |
         if (at.zeros) {
             const float none[8] = {};
             const int pieces = (p.N + 7) / 8;
-            for (int r = at.m0 + (int)blockIdx.x - tiles; r < at.m_end; r += gridDim.x - tiles)
-                for (int i = threadIdx.x; i < pieces; i += L::THREADS * PARTS) store_results<8>(p, r, i * 8, none);
+            const NoRows rows(p, at);
+            for (int i = (int)blockIdx.x - tiles; i < rows.count; i += gridDim.x - tiles)
+                for (int j = threadIdx.x; j < pieces; j += L::THREADS * PARTS) store_results<8>(p, rows[i], j * 8, none);
             return;
         }
     } else {
@@ -613,10 +621,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_few_kernel(Fp8Problem p, i
         at = place_of<16 * MT>(p.offsets, p.E, p.M, lane, [&](int) { return id / tiles_n; });
         if (at.zeros) {
             const float none[4] = {};
+            const NoRows rows(p, at);
             const int step = (slots - (id / tiles_n - at.e)) * 16 * MT;
-            for (int r = at.m0 + at.e * 16 * MT; r < at.m_end; r += step)
+            for (int r = at.e * 16 * MT; r < rows.count; r += step)
                 for (int i = threadIdx.x; i < 16 * MT * (WIDTH / 4); i += 64 * FEW_WAVES)
-                    if (r + i / (WIDTH / 4) < at.m_end) store_results<4>(p, r + i / (WIDTH / 4), id % tiles_n * WIDTH + i % (WIDTH / 4) * 4, none);
+                    if (r + i / (WIDTH / 4) < rows.count) store_results<4>(p, rows[r + i / (WIDTH / 4)], id % tiles_n * WIDTH + i % (WIDTH / 4) * 4, none);
             return;
         }
     }

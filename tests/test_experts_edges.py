@@ -48,6 +48,24 @@ def test_host_takes_a_list_of_rows_of_an_empty_source(launches):
     assert [(c["rc"], c["launches"]) for c in launches(refused)] == [(1, 0)] * len(refused)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,K,R", [(130, 200, 60), (2056, 384, 700), (4104, 1100, 4000)])
+@pytest.mark.parametrize("fast", [False, True])
+def test_experts_whose_rows_begin_later(N, K, R, fast):
+    """A part of the experts' offsets: the rows ahead of its first expert are no expert's either, zeros like those behind its last."""
+    g = torch.Generator("cuda").manual_seed(R)
+    a, sa = some_rows(g, R, K), torch.rand(-(-K // 128), R, generator=g, device="cuda") + 0.5
+    w, sw = some_rows(g, 2 * N, K).view(2, N, K), torch.rand(2, -(-N // 128), -(-K // 128), generator=g, device="cuda") + 0.5
+    for off in ([R // 4, R // 2, R - 7], [R // 3, R // 3, R // 3], [R, R, R], [1, R - 1, R]):
+        out = torch.full((R, N), float("nan"), device="cuda")
+        xp.gemm_fp8_experts(a, sa, w, sw, torch.tensor(off, dtype=torch.int32, device="cuda"), dtype=torch.float32, fast_sums=fast, out=out)
+        assert not out[:off[0]].any() and not out[off[2]:].any()
+        for e in range(2):
+            i, j = off[e], off[e + 1]
+            want, slack = product_64(a[i:j], sa[:, i:j], w[e], sw[e])
+            assert ((out[i:j].double() - want).abs() <= slack + 2.0 ** -24 * want + (CUT * want if fast else 0)).all()
+
+
 def example():
     import importlib.util
     spec = importlib.util.spec_from_file_location("experts_layer", os.path.join(ROOT, "examples", "experts_layer.py"))
