@@ -106,7 +106,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteProblem p)
         }
         if (p.group_top == 2 && b > none) {   // (of two that are to be had)
             auto value = [](int key) { return __builtin_bit_cast(float, key ^ (key >> 31 & 0x7fffffff)); };
-            a = order_key(value(a) + value(b));
+            a = order_key(fmaxf(value(a) + value(b), -FLT_MAX));   // (of two lowest numbers: not -infinity, which is a group of none)
         }
         int ahead = 0;   // groups that come before mine
         for (int o = 0; o < p.groups; ++o) {

@@ -687,3 +687,23 @@ def test_gate_backward_of_many_rows(size, apart, dtype):
     tiny = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}[dtype]
     assert ((frame[:, :2 * cols].double() - want).abs() <= slack + step * want.abs() + tiny).all()
     assert (frame[:, 2 * cols:] == 7).all()
+
+
+# ---- routing ------------------------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("each", [2, 5, 40])
+def test_groups_masked_by_the_lowest_number(each, score):
+    """Experts whose bias is the lowest finite number are to be had, so a group of them comes before one of none, and its best two's sum is no minus infinity."""
+    lowest = torch.finfo(torch.float32).min
+    x = torch.zeros(3, 4 * each, device="cuda")
+    x[:2, :each] = -float("inf")            # group 0: none to be had (of the last token all)
+    bias = torch.zeros(4 * each, device="cuda")
+    bias[2 * each:] = lowest
+    ids, w = xp.route_experts(x, min(2 * each, 50), score=score, bias=bias, groups=4, kept=2, group_top=2)
+    some_of = ids[0].tolist()
+    assert some_of == list(range(each, each + len(some_of))) and (w[0] > 0).all()   # group 1, then group 2
+    assert ids[2].tolist() == list(range(len(some_of)))
+    x[1, each:2 * each] = -float("inf")      # only masked ones are left: groups 2 and 3
+    ids, w = xp.route_experts(x, min(2 * each, 50), score=score, bias=bias, groups=4, kept=2, group_top=2)
+    assert ids[1].tolist() == list(range(2 * each, 2 * each + min(2 * each, 50))), ids[1]
