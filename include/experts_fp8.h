@@ -61,7 +61,8 @@ int silu_gate_backward(int rows, int cols, const void *x, long long ldx, const v
  * cuts each of eight neighbouring products (k = 8 i ... 8 i + 7) towards zero to a multiple of 2^-13 of the largest one's power of two: a result is then up to
  * 7 * 2^-13 (8.5e-4) of the sum of its terms' magnitudes off, more than rounding to float16; with values of one size and random sign 1.5e-5 of the result in the mean, a
  * hundredth of rounding to bfloat16, but losses of terms of one sign add up.  A [M][K], sa [ceil(K/128)][M] dense.  b_rows == 0: sb[n / 128][b] ([ceil(N/128)][ceil(K/128)],
- * weights); != 0: sb[b][n] ([ceil(K/128)][N]).  Scales are any f32.  Gradients are the same product: of the input with the
+ * weights); != 0: sb[b][n] ([ceil(K/128)][N]).  Scales are any f32 whose products sa * sb are
+ * finite too.  Gradients are the same product: of the input with the
  * weights quantised transposed, of the weights with both operands quantised by columns. */
 int gemm_fp8_nt(int M, int N, int K, const uint8_t *A, long long lda, const float *sa, const uint8_t *B, long long ldb, const float *sb, int b_rows,
                 void *C, long long ldc, int out_type, int fast_sums, void *stream);
@@ -81,7 +82,7 @@ int gemm_fp8_experts_grad(int R, int E, int N, int K, const uint8_t *A, long lon
  * s = softmax(logits) (sigmoid != 0: 1 / (1 + exp(-logits))) over a token's E experts; an expert whose logit is -infinity or NaN
  * is not to be had and has no part in the softmax; +infinity counts as the largest finite value.  Choice by c = s + bias
  * (bias: f32 [E] or NULL; an expert whose c is -infinity or NaN is not to be had): of `groups` equal
- * groups of neighbouring experts the `kept` of highest score (the sum of the group_top (1 or 2) largest c of those to be had) remain, of their
+ * groups of neighbouring experts the `kept` of highest score (the sum of the group_top (1 or 2) largest c of those to be had, the lowest finite number at least) remain, of their
  * experts the k of largest c, in falling order; ties go to the lower index.  ids [T][k] int32, -1 where fewer are to be had.
  * weights [T][k] f32: s of the chosen (without the bias), / (their sum + 1e-20) if renormalise, * factor; 0 beside -1.
  * E up to EXPERTS_MOST, k up to EXPERTS_MOST_CHOICES and to E, groups up to 64. */

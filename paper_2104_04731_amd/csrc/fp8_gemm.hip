@@ -809,10 +809,18 @@ hipError_t launch_fp8_gemm(const Fp8Problem &p, GemmKind kind, hipStream_t st)
     // (and a launch need not hold as many of the smaller: 1024 weight gradients of 8192 x 8192 ask for 2^24)
     if ((area >= (kind == GEMM_EXPERTS ? 6e6 : 8e6) && rows > 64 && (p.fast_sums || depth >= 4)) || !fits_launch(tiles_of(p, kind, 64, 64), 256))
         return p.fast_sums ? launch_tiles<128, 128, 2, 2, 1, true>(p, kind, way, st) : launch_tiles<128, 128, 2, 2, 1, false>(p, kind, way, st);
-    // Tiles for no more than the compute units and a deep sum: in four parts to a workgroup, which bring in more at a time (us, one part | four: 300 x 1024,
-    // depth 4096 13.4 | 10.1; 512 x 512, 8192 31 | 18.6; 512 x 512, 1024 5.6 | 5.7 and in 32 bits 7.3 | 6.9; of more tiles 1000 x 2048, 2048 10.0 | 13.9).
+    // Tiles for no more than the compute units and a deep sum: in four parts to a workgroup, which bring in more at a time; of more tiles one part (1000 x 2048, depth 2048
+    // 10.0 | 13.9).  From which depth on four take less depends on what a step costs: 16 waves leave 128 registers each, of which 32-bit sums spill 17 where B has a scale
+    // for each row and 7 in weight gradients, and rows off 16 bytes come in through registers (us, one part | four; depth in blocks):
+    //   blocks                          8            12           16           32
+    //   512 x 512, fast sums        5.5 |  5.5   6.8 |  6.5   8.1 |  7.3  13.2 | 10.1      off 16 bytes   7.0 |  6.9   8.9 |  9.1  10.8 | 10.7  18.8 | 17.3
+    //   32-bit sums                 7.2 |  7.0   9.3 |  8.1  11.3 |  9.1  19.7 | 13.4                     8.5 |  8.7  11.3 | 10.5  14.0 | 12.2  25.0 | 19.3
+    //   B with a scale for a row    7.2 |  7.8   9.3 |  9.1  11.4 | 10.4  19.9 | 15.6                     8.4 | 10.1  11.1 | 11.8  13.7 | 13.4  24.6 | 20.5
+    //   gradients, 2 of 512 x 512   7.7 |  9.5               11.9 | 12.6  20.6 | 18.7                     9.0 | 10.8               14.8 | 14.0  25.5 | 20.9
+    // Rows too far apart for either go row by row, which is one part's work.
     const double tiles = ((p.M + 63) / 64 + (kind == GEMM_EXPERTS ? p.E / 2 : 0)) * (double)((p.N + 63) / 64) * (kind == GEMM_GRAD ? p.E : 1);
-    if (tiles <= 256 && depth >= (p.fast_sums ? 12 : 8))
+    const int from = way == WAY_ROWS ? 0x7fffffff : way == WAY_TRANSFERS ? (p.fast_sums ? 12 : kind == GEMM_GRAD ? 32 : p.b_rows ? 12 : 8) : p.fast_sums ? 32 : p.b_rows ? 16 : 12;
+    if (tiles <= 256 && depth >= from)
         return p.fast_sums ? launch_tiles<64, 64, 2, 2, 4, true>(p, kind, way, st) : launch_tiles<64, 64, 2, 2, 4, false>(p, kind, way, st);
     return p.fast_sums ? launch_tiles<64, 64, 2, 2, 1, true>(p, kind, way, st) : launch_tiles<64, 64, 2, 2, 1, false>(p, kind, way, st);
 }

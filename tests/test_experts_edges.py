@@ -451,7 +451,7 @@ SIZES = {
     (256, 1): dict(dense=(3900, 4104, 1100), experts=((1700, 0, 2296), 4104, 1100), grad=((700, 0, 901), 2300, 2200)),
     (128, 1): dict(dense=(2900, 3000, 650), experts=((900, 2, 0, 1598), 2600, 650), grad=((300, 0, 900, 901), 1100, 2050)),
     (64, 1): dict(dense=(257, 300, 390), experts=((70, 0, 230), 300, 390), grad=((300, 0, 389), 130, 200)),
-    (64, 4): dict(dense=(300, 520, 2000), experts=((70, 3, 227), 520, 2000), grad=((1605, 1695), 130, 200)),
+    (64, 4): dict(dense=(300, 520, 4100), experts=((70, 3, 227), 520, 4100), grad=((4205, 4090), 130, 200)),
 }
 FEW = {(mt, split): dict(dense=(rows, 300, depth), experts=(counts, 140, depth))
        for mt, rows, counts in ((1, 7, (9, 0, 17, 3)), (2, 20, (41, 0, 30, 33))) for split, depth in ((1, 200), (4, 400), (8, 1300))}
@@ -468,6 +468,8 @@ def all_cases():
                     out += [((tile, parts), kind, b_rows, 1, TRANSFERS, size)] if fast else []
                     continue
                 out += [((tile, parts), kind, b_rows, fast, way, size) for way in (TRANSFERS, REGISTERS)]
+                if parts == 4:   # (rows too far apart are one part's work)
+                    continue
                 if tile == 128 and kind != EXPERTS:   # (few columns, whose rows lie far apart, and many rows)
                     size = (120000, 70, 650) if kind == DENSE else ((300, 0, 900, 901), 30000, 70)
                 out.append(((tile, parts), kind, b_rows, fast, ROWS, size))
@@ -707,3 +709,20 @@ def test_groups_masked_by_the_lowest_number(each, score):
     x[1, each:2 * each] = -float("inf")      # only masked ones are left: groups 2 and 3
     ids, w = xp.route_experts(x, min(2 * each, 50), score=score, bias=bias, groups=4, kept=2, group_top=2)
     assert ids[1].tolist() == list(range(2 * each, 2 * each + min(2 * each, 50))), ids[1]
+
+
+def parts_of(call):
+    import re
+    m = re.search(r"fp8_tile_kernelILi(\d+)ELi\d+ELi\d+ELi\d+ELi(\d+)E", call["kernel"])
+    return int(m.group(1)), int(m.group(2))
+
+
+def test_host_depth_in_parts_where_that_is_faster(launches):
+    """Four parts or one, at sizes where the other takes longer (us, one | four)."""
+    four = [dense_call(512, 512, 1536), dense_call(512, 512, 2048, fast=1), dense_call(512, 512, 2048, b_rows=1), dense_call(512, 512, 2048, on16=False), dense_call(512, 512, 4096, fast=1, on16=False),
+            dense_call(512, 512, 4096, b_rows=1, on16=False), grad_call(2 * 4096, 2, 512, 512), grad_call(4 * 2048, 4, 512, 512, fast=1), grad_call(2 * 4096, 2, 512, 512, on16=False, ld=8195),
+            experts_call(300, 300, 4, 512, 2048, rows=False)]    # 9.3 | 8.1, 8.1 | 7.3, 11.4 | 10.4, 14.0 | 12.2, 18.8 | 17.3, 24.6 | 20.5, 20.6 | 18.7, 9.1 | 8.6, 25.5 | 20.9, 11.6 | 9.6
+    one = [dense_call(512, 512, 1024, b_rows=1), grad_call(4 * 1024, 4, 512, 256), grad_call(16 * 2048, 16, 256, 256), dense_call(512, 512, 1536, fast=1, on16=False),
+           dense_call(1000, 1000, 1536, b_rows=1, on16=False), dense_call(512, 512, 2048, ldb=FAR)]                # 7.2 | 7.8, 7.6 | 9.6, 12.3 | 13.6, 8.9 | 9.1, 11.8 | 12.9; (one part works)
+    got = [parts_of(c) for c in launches(four + one)]
+    assert got == [(64, 4)] * len(four) + [(64, 1)] * len(one)
