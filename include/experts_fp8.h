@@ -57,13 +57,13 @@ int silu_gate_backward(int rows, int cols, const void *x, long long ldx, const v
 
 /* ---- products ------------------------------------------------------------------------------------------------------
  * C[m][n] = sum over blocks b of 128 of K:  sa[b][m] * sb * (sum over k in b of A[m][k] * B[n][k]), 32-bit sums,
- * rounded once to out_type.  fast_sums != 0: the sum within a block may be taken by the 8-bit matrix instruction, up to twice as fast, which
- * cuts each of eight neighbouring products (k = 8 i ... 8 i + 7) towards zero to a multiple of 2^-13 of the largest one's power of two: a result is then up to
- * 7 * 2^-13 (8.5e-4) of the sum of its terms' magnitudes off, more than rounding to float16; with values of one size and random sign 1.5e-5 of the result in the mean, a
- * hundredth of rounding to bfloat16, but losses of terms of one sign add up.  A [M][K], sa [ceil(K/128)][M] dense.  b_rows == 0: sb[n / 128][b] ([ceil(N/128)][ceil(K/128)],
- * weights); != 0: sb[b][n] ([ceil(K/128)][N]).  Scales are any f32 whose products sa * sb are
- * finite too.  Gradients are the same product: of the input with the
- * weights quantised transposed, of the weights with both operands quantised by columns. */
+ * rounded once to out_type.  A [M][K], sa [ceil(K/128)][M] dense.  b_rows == 0: sb[n / 128][b] ([ceil(N/128)][ceil(K/128)], weights);
+ * != 0: sb[b][n] ([ceil(K/128)][N]).  Scales are any f32 whose products sa * sb are finite too.  Gradients are the same product: of the
+ * input with the weights quantised transposed, of the weights with both operands quantised by columns.
+ * fast_sums != 0: the sum within a block may be taken by the 8-bit matrix instruction, up to twice as fast, which cuts each of eight
+ * neighbouring products (k = 8 i ... 8 i + 7) towards zero to a multiple of 2^-13 of the largest one's power of two.  A result is then up
+ * to 7 * 2^-13 (8.5e-4) of the sum of its terms' magnitudes off, which is more than rounding to float16; with values of one size and random
+ * sign 1.5e-5 of the result in the mean, a hundredth of rounding to bfloat16, but losses of terms of one sign add up. */
 int gemm_fp8_nt(int M, int N, int K, const uint8_t *A, long long lda, const float *sa, const uint8_t *B, long long ldb, const float *sb, int b_rows,
                 void *C, long long ldc, int out_type, int fast_sums, void *stream);
 /* A weight matrix for each expert.  Row r of C, offsets[e] <= r < offsets[e + 1], is the product of A's row r -- with rows

@@ -247,7 +247,7 @@ enum Way : int { WAY_ROWS = 0, WAY_REGISTERS = 1, WAY_TRANSFERS = 2 };
 // 243, 2.26, between other work; 229 of zeros) and 8192 x 4096, depth 4096, in 144; 32768 rows of 64 experts, 2048 x 2048, in 222 (1.24 PFLOP/s: a fifth of the tiles' rows
 // are no expert's, and start and results are a quarter of 16 steps).  In 32-bit sums 8192 x 4096, depth 4096, in 287 us (0.96 PFLOP/s: the widening of both
 // operands goes through the vector units of the same waves); 16 weight gradients of 1024 x 2048 over 10000 rows in 102 (134 MB of results).  Of few rows it is the weights'
-// bytes that count: 16 tokens of 4 experts each of 64, 2048 x 2048, in 26 to 37 us (173 MB, of which the last level cache holds more or less).
+// bytes that count: 16 tokens of 4 experts each of 64, 2048 x 2048, in 26 to 38 us (173 MB, of which the last level cache holds more or less; 42 where it holds nothing).
 template <int TM, int TN, int WM, int WN, int PARTS, GemmKind KIND, bool BROWS, bool FAST>
 __global__ __launch_bounds__(64 * WM * WN * PARTS, TM * TN <= 64 * 64 && (FAST || !BROWS || PARTS > 1) ? 4 : 2) void fp8_tile_kernel(Fp8Problem p, int slots, int tiles_n, Way way)
 {
@@ -788,11 +788,15 @@ hipError_t launch_fp8_gemm(const Fp8Problem &p, GemmKind kind, hipStream_t st)
     const double rows = kind == GEMM_EXPERTS ? (double)p.M / p.E : p.M;   // of a weight matrix, in the mean
     const int depth = blocks_of(p.K) / (kind == GEMM_GRAD ? p.E : 1);
     // Few rows: the kernel without tiles has the shorter start and step, but reads A again for 16 columns each and moves bytes more slowly; so it is for
-    // weights that take no longer than a tile's steps (us, few | tiles; M x N, depth, or tokens, experts of each token and of all, N, depth):
-    //   1 x 32768, 4096      30 | 36      16 x 65536, 2048  36 | 26      1, 4 of 64, 1024, 2048    5.4 |  9.6      128, 4 of 64, 1024, 2048   45 | 22
-    //   20 x 4096, 4096     8.4 | 10.7    28 x 16384, 4096  25 | 15.5    16, 2 of 16, 1024, 2048  10.2 | 11.1      16, 4 of 64, 2048, 2048    33 | 30
-    // Rows that are not on 16 bytes cost it twice as much: 64, 2 of 16, 512, 1981  17.3 | 14.6.  Of over 32 rows tiles are level or better (33 x 16384, 4096  37 | 15) but
-    // for the smallest (33 x 300, 777  6.5 | 8.8).
+    // weights that take no longer than a tile's steps.  Where that ends depends on where the weights are, since the tiles move bytes faster from the last level cache: from memory
+    // at a cost (below) of some 4.5e6 a step, from the cache at 2e6 with fast sums and 3e6 in 32 bits; 2.5e6 lies between (us, few | tiles in 32-bit sums, weights from memory, then from the
+    // cache; rows x N, depth, or tokens, experts of each and of all, N, depth):
+    //   1.1e6   1, 4 of 64, 2048, 2048    7.8 | 13.9    6.2 | 12.3       3.1e6   12 x 16384, 4096         18.1 | 21.3   16.8 | 15.7
+    //   2.1e6   2, 4 of 64, 2048, 2048   10.7 | 14.4    9.6 | 13.7       4.2e6   8 x 32768, 4096          30.1 | 35.5   27.6 | 25.6
+    //   2.1e6   8 x 16384, 4096          17.8 | 21.5   15.9 | 15.9       5.2e6   20 x 16384, 4096         22.7 | 21.6   21.2 | 16.2
+    //   3.1e6   64, 2 of 16, 1024, 2048  12.0 | 14.2   11.3 | 11.7       9.1e6   8, 6 of 64, 1408, 2048   28.7 | 27.3   27.1 | 24.0
+    // Rows that are not on 16 bytes cost it twice as much: 64, 2 of 16, 512, 1981 (1.5e6) 12.9 | 17.6, 128 of them (2.0e6) 22.5 | 19.0.  Of over 32 rows tiles are level or better
+    // (33 x 16384, 4096  37 | 15) but for the smallest (33 x 300, 777  6.5 | 8.8).
     if (kind != GEMM_GRAD && rows <= 32) {
         const double weights = (kind == GEMM_EXPERTS ? fmin(p.M, p.E) : 1.) * p.N * p.K;   // bytes of those asked for
         const double cost = kind == GEMM_EXPERTS ? weights * (1 + rows / 16) : weights * rows / 8;
